@@ -21,6 +21,11 @@
  *                    cut, and the extra token drawn from the normalised residual
  *                    max(p - q, 0), or from p when the whole block survives.
  *
+ * Around the paged cache: sv_rope_append rotates queries and keys by positions on several
+ * axes and appends (instead of sv_append_kv), sv_window_attn attends within a sliding window
+ * and to the first tokens (instead of sv_verify_attn), and sv_fork_pages, sv_reserve_pages,
+ * sv_release_pages, sv_compact_pages and sv_copy_pages keep the page table between rounds.
+ *
  * On the drafter's side, sv_draft_stats gives each draft row its softmax
  * normaliser and the confidence c_t the budget takes; sv_spec_accept_stats is the
  * acceptance that uses those normalisers instead of re-reading the draft rows.
@@ -277,6 +282,209 @@ sv_status sv_prepare_round(const sv_budget_desc* bdesc, const float* conf, int32
                            const int32_t* block_tokens, const int32_t* ctx_lens, int32_t* tokens,
                            int32_t* positions, int32_t* kv_lens, const sv_attn_desc* adesc, void* attn_ws,
                            size_t attn_ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------- */
+/* Rotary positions with several axes, on the way into the cache              */
+/* ------------------------------------------------------------------------- */
+#define SV_MAX_ROPE_AXES 4
+
+typedef enum {
+    SV_ROPE_BLOCKS = 0, /* the first section[0] pairs turn with axis 0, the next section[1] with axis 1, ... */
+    SV_ROPE_CYCLE = 1   /* pair p turns with axis a = p mod num_axes while p / num_axes < section[a],
+                           else with axis 0                                                                */
+} sv_rope_order;
+typedef enum {
+    SV_ROPE_HALVES = 0,  /* pair p is dims (p, p + rot_dim / 2) */
+    SV_ROPE_ADJACENT = 1 /* pair p is dims (2p, 2p + 1)         */
+} sv_rope_pairing;
+
+typedef struct {
+    int32_t num_reqs;          /* R in [1, 65535]                                               */
+    int32_t total_max;         /* rows allocated in q / k_new / v_new / positions / q_out; times the heads < 2^31 */
+    int32_t num_q_heads;       /* Hq                                                            */
+    int32_t num_kv_heads;      /* Hkv                                                           */
+    int32_t head_dim;          /* d; d * element size a multiple of 16 bytes, d <= 1024          */
+    int32_t rot_dim;           /* rotated dims, even, in [2, d]; dims from rot_dim on pass through */
+    int32_t num_axes;          /* position axes, 1..4 (time, height, width, ...)                */
+    int32_t section[SV_MAX_ROPE_AXES]; /* pairs of each axis, >= 0; they sum to rot_dim / 2      */
+    int32_t order;             /* sv_rope_order                                                 */
+    int32_t pairing;           /* sv_rope_pairing                                               */
+    int32_t q_stride;          /* elements from a row of q to the next, 0 = Hq * d (rows of a fused */
+    int32_t k_stride;          /* projection lie further apart); k_new and v_new: 0 = Hkv * d.  */
+    int32_t v_stride;          /* At least the row, a multiple of 16 bytes                      */
+    int32_t page_size;         /* P, a power of two in [1, 4096]                                */
+    int32_t max_pages_per_req; /* columns of page_table                                         */
+    int32_t num_pages;         /* pages in each cache                                           */
+    int32_t dtype;             /* sv_dtype of the rows and the caches                           */
+    float scale;               /* factor of the rotated dims (long-context schemes scale them); 0 means 1 */
+} sv_rope_desc;
+
+/*
+ * sv_rope_append -- rotary position embedding of a packed batch's queries and keys, and the
+ * append of its keys and values to the paged cache: sv_append_kv for rows as the projection
+ * leaves them. Row r = qo_indptr[i] + j (any number of rows per request: one new token, a
+ * verify block, a prompt) at positions x_a = positions[a][r]:
+ *     pair p of axis a(p):  t = x_a * inv_freq[p],
+ *     (u, v) -> scale * (u cos t - v sin t, v cos t + u sin t)
+ * in every head of q and k_new; q_out[r] gets the query, position s = ctx_lens[i] + j of
+ * request i gets the key and (unchanged) value: page page_table[i][s / P], slot s % P.
+ * The rotary positions may differ from s (an image's tokens share a time position).
+ * The angle is computed in fp64 (positions beyond 2^24 keep their fraction of a turn), sine
+ * and cosine and the rotation in fp32, rounded once to the storage type.
+ * A row that no request owns is untouched in q_out, and so are all rows of a request whose
+ * rows are not inside [0, total_max). The cache is not written for a row with a page id outside
+ * [0, num_pages), a page column outside [0, max_pages_per_req) or ctx_lens[i] < 0; its query
+ * is rotated all the same. qo_indptr is non-decreasing. q_out may be q itself (with
+ * q_stride 0 or Hq * d); other overlaps of inputs and outputs are not allowed. Two rows that map
+ * to the same slot race.
+ * q [total_max, Hq, d], k_new, v_new [total_max, Hkv, d], rows q_stride / k_stride / v_stride apart
+ * positions [num_axes, total_max] int32; inv_freq [rot_dim / 2] fp64 (8-byte aligned), radians
+ * per position; page_table [R, max_pages_per_req]; qo_indptr [R+1]; ctx_lens [R] int32
+ * q_out [total_max, Hq, d] dense (sv_verify_attn's q); k_cache, v_cache [num_pages, Hkv, P, d]
+ */
+sv_status sv_rope_append(const sv_rope_desc* desc, const void* q, const void* k_new, const void* v_new,
+                         const int32_t* positions, const double* inv_freq, const int32_t* page_table,
+                         const int32_t* qo_indptr, const int32_t* ctx_lens, void* q_out, void* k_cache,
+                         void* v_cache, void* stream);
+
+/* ------------------------------------------------------------------------- */
+/* Attention with a sliding window and visible first tokens                   */
+/* ------------------------------------------------------------------------- */
+typedef struct {
+    sv_attn_desc attn; /* as in sv_verify_attn; kv_split: visible tokens per work item      */
+    int32_t window;    /* W >= 1: a row sees its own position and the W - 1 before it       */
+    int32_t sinks;     /* S >= 0: and the first S positions of its request                  */
+} sv_window_desc;
+
+/*
+ * sv_window_attn -- sv_verify_attn of a layer with a sliding window: the row at position
+ * p = L_i + j of request i attends to the keys s <= p with s < S or s > p - W. From one row
+ * per request (a new token) to 16. Arguments, layouts and results as in sv_verify_attn.
+ * Pages that hold no such key of any of the request's rows are never read: their entries of
+ * page_table may be -1 (sv_release_pages gives them back). A key that a row should see but
+ * whose page id is outside [0, num_pages) or whose column is outside the table counts as
+ * masked; a row without any key left gets out = 0 and lse = -inf. NaN and infinities in keys and
+ * values that a row does not see do not reach it. Rows that no request owns are untouched, and so are those of a request with k_i outside [1, block],
+ * rows outside [0, total_q_max) or kv_lens[i] < k_i; kv_lens[i] above max_kv_len counts as
+ * max_kv_len.
+ * ws: scratch of sv_window_attn_workspace_size(desc) bytes (0 for many calls), overwritten.
+ * bf16 runs on MFMA with fp32 accumulation. The same call on the same inputs gives the same
+ * bits, and a request's results do not depend on the other requests' lengths.
+ */
+sv_status sv_window_attn(const sv_window_desc* desc, const void* q, const void* k_cache, const void* v_cache,
+                         const int32_t* page_table, const int32_t* qo_indptr, const int32_t* kv_lens, void* out,
+                         float* lse, void* ws, size_t ws_bytes, void* stream);
+size_t sv_window_attn_workspace_size(const sv_window_desc* desc);
+
+/* ------------------------------------------------------------------------- */
+/* Pages of the cache: fork, reserve with copy-on-write, release, compact, copy */
+/* ------------------------------------------------------------------------- */
+#define SV_MAX_RESERVE_REQS 4096 /* R of sv_reserve_pages */
+
+typedef struct {
+    int32_t num_reqs;          /* R in [1, 65535] rows of the page table            */
+    int32_t max_pages_per_req; /* columns of the page table; R * columns < 2^31     */
+    int32_t num_pages;         /* pages in the cache, <= 2^24                       */
+    int32_t page_size;         /* P, a power of two in [1, 4096]                    */
+} sv_pages_desc;
+
+/*
+ * The pages of a cache are counted: ref[p] is the number of page-table entries that hold page
+ * p, over all tables of the cache; 0 means free. page_table[i][c] holds positions c * P ..
+ * (c + 1) * P - 1 of request i; an id outside [0, num_pages) (-1) means no page. All of it is
+ * device memory of the caller; every call is asynchronous on its stream, the host never
+ * waits for a count. The results of these calls are the same whatever order the GPU works in.
+ * With counts that do not fit the tables the results are unspecified, but every access stays
+ * in bounds.
+ */
+
+/*
+ * sv_fork_pages -- the table of the next batch from that of the last: row i of table_out
+ * shares the pages of row parent[i] of table_in, which holds lens_in[parent[i]] tokens:
+ *     table_out[i][c] = table_in[parent[i]][c] for c * P < lens_in[parent[i]], else -1
+ *     lens_out[i] = lens_in[parent[i]]
+ * A parent may be taken any number of times (samples of a prompt, beams) or not at all
+ * (retired requests); parent[i] outside [0, rows_in) gives an empty row of length 0, and so does
+ * a parent with lens_in < 0. table_out
+ * replaces table_in: ref counts the entries of table_out and no more those of table_in
+ * (pages that nobody holds any more become free); table_in itself is left as it was.
+ * table_in [rows_in, max_pages_per_req], lens_in [rows_in], parent [R], table_out
+ * [R, max_pages_per_req], lens_out [R], ref [num_pages] int32. Inputs and outputs must not
+ * overlap (checked for the tables).
+ */
+sv_status sv_fork_pages(const sv_pages_desc* desc, int32_t rows_in, const int32_t* table_in,
+                        const int32_t* lens_in, const int32_t* parent, int32_t* table_out, int32_t* lens_out,
+                        int32_t* ref, void* stream);
+
+/*
+ * sv_reserve_pages -- makes positions ctx_lens[i] .. new_lens[i] - 1 of every request
+ * writable: each of their columns gets a page of its own. In the order of the requests, and of
+ * the columns of a request, over columns ctx / P .. ceil(new / P) - 1 (none when new <= ctx):
+ *   - a column without a page takes the free page of the lowest id;
+ *   - a column whose page is shared (ref > 1 at this point of the order) takes the free page of the
+ *     lowest id too and gives up its share. Where it is the page that holds position ctx
+ *     and ctx % P > 0, the committed tokens in it have to be copied:
+ *     (old id, new id, ctx % P) is appended to copy_src / copy_dst / copy_tokens.
+ *   - a page that the request holds alone stays (the last of its sharers keeps it).
+ * Pages that are free when the call begins are taken. A request is served whole or not at
+ * all: the first for which too few free pages are left, or with ctx_lens[i] < 0 or more
+ * columns than the table has, and all requests after it stay as they were.
+ * info [4] int32 out: requests served (a prefix of the batch), pages taken, copies, free
+ * pages left. copy_src, copy_dst, copy_tokens [R] int32 out; entries past the copies untouched.
+ * ws: scratch of sv_reserve_pages_workspace_size(desc) bytes. R <= 4096.
+ */
+sv_status sv_reserve_pages(const sv_pages_desc* desc, int32_t* page_table, int32_t* ref, const int32_t* ctx_lens,
+                           const int32_t* new_lens, int32_t* copy_src, int32_t* copy_dst, int32_t* copy_tokens,
+                           int32_t* info, void* ws, size_t ws_bytes, void* stream);
+size_t sv_reserve_pages_workspace_size(const sv_pages_desc* desc);
+
+/*
+ * sv_release_pages -- gives back the pages that no row at position lens[i] or later needs:
+ * columns c with c * P >= lens[i] (rejected drafts; lens[i] <= 0: the whole request) and, with
+ * window W > 0 and `sinks` S, columns of positions that are all >= S and <= lens[i] - W
+ * (sv_window_attn with this window never reads them again). Their entries become -1 and
+ * their counts go down. window = 0: no window.
+ */
+sv_status sv_release_pages(const sv_pages_desc* desc, int32_t window, int32_t sinks, int32_t* page_table,
+                           int32_t* ref, const int32_t* lens, void* stream);
+
+/*
+ * sv_compact_pages -- moves the pages in use to the low end of the cache: the k-th highest
+ * page in use goes to the k-th lowest free page, for k = 0, 1, .. while the free one
+ * lies below, at most max_moves of them (0: all). page_table and ref follow; the caller
+ * copies the data with sv_copy_pages(move_src, move_dst, &info[0]) in every layer before
+ * the pages are used. page_table must hold all tables of the cache (R rows). move_src,
+ * move_dst [max_moves, or num_pages / 2 when that is less or max_moves is 0] int32 out,
+ * entries past the moves untouched; info [2] int32 out: moves, pages in use.
+ * ws: scratch of sv_compact_pages_workspace_size(desc) bytes.
+ */
+sv_status sv_compact_pages(const sv_pages_desc* desc, int32_t max_moves, int32_t* page_table, int32_t* ref,
+                           int32_t* move_src, int32_t* move_dst, int32_t* info, void* ws, size_t ws_bytes,
+                           void* stream);
+size_t sv_compact_pages_workspace_size(const sv_pages_desc* desc);
+
+typedef struct {
+    int32_t max_copies;   /* entries of src / dst (the device count may be less)   */
+    int32_t num_layers;   /* layers whose caches follow each other, >= 1           */
+    int32_t num_kv_heads; /* Hkv                                                   */
+    int32_t head_dim;     /* d; d * element size a multiple of 16 bytes            */
+    int32_t page_size;    /* P, a power of two in [1, 4096]                        */
+    int32_t num_pages;    /* pages in each layer's cache                           */
+    int32_t dtype;        /* sv_dtype of the caches                                */
+    int64_t layer_stride; /* elements from a layer's cache to the next, 0 = dense; a multiple of 16 bytes */
+} sv_copy_desc;
+
+/*
+ * sv_copy_pages -- page dst[e] of the K and V caches becomes a copy of page src[e] in every
+ * layer, for e < min(*count, max_copies): whole pages, or their first tokens[e] slots (tokens not
+ * NULL, clamped to [0, P]; the other slots of dst[e] stay). An entry with an id outside
+ * [0, num_pages) is skipped. No page may be a destination twice, or a source and a
+ * destination (lists of sv_reserve_pages and sv_compact_pages are so).
+ * src, dst [max_copies], tokens [max_copies] or NULL, count [1] int32, device memory;
+ * k_cache, v_cache [num_layers, num_pages, Hkv, P, d].
+ */
+sv_status sv_copy_pages(const sv_copy_desc* desc, const int32_t* src, const int32_t* dst, const int32_t* tokens,
+                        const int32_t* count, void* k_cache, void* v_cache, void* stream);
 
 /* ------------------------------------------------------------------------- */
 /* Speculative acceptance (rejection-sampling verification, Sec. 1; the       */

@@ -18,7 +18,10 @@ SV_OK, SV_ERR_INVALID_ARG, SV_ERR_UNSUPPORTED, SV_ERR_WORKSPACE, SV_ERR_HIP = ra
 SV_F32, SV_BF16 = 0, 1
 SV_LOGITS, SV_PROBS = 0, 1
 SV_BUDGET_FIXED, SV_BUDGET_COST = 0, 1
+SV_ROPE_BLOCKS, SV_ROPE_CYCLE = 0, 1
+SV_ROPE_HALVES, SV_ROPE_ADJACENT = 0, 1
 SV_MAX_RATIOS = 8
+SV_MAX_ROPE_AXES = 4
 
 # every symbol the header declares (checked by the ABI test)
 EXPORTED = ("sv_alloc_budget", "sv_pack_verify", "sv_append_kv", "sv_verify_attn", "sv_verify_attn_workspace_size",
@@ -26,7 +29,9 @@ EXPORTED = ("sv_alloc_budget", "sv_pack_verify", "sv_append_kv", "sv_verify_attn
             "sv_spec_accept", "sv_spec_accept_workspace_size", "sv_spec_accept_noalloc", "sv_spec_accept_debug",
             "sv_spec_accept_stats",
             "sv_draft_stats",
-            "sv_draft_stats_workspace_size", "sv_status_string", "sv_last_error", "sv_abi_version")
+            "sv_draft_stats_workspace_size", "sv_rope_append", "sv_window_attn", "sv_window_attn_workspace_size",
+            "sv_fork_pages", "sv_reserve_pages", "sv_reserve_pages_workspace_size", "sv_release_pages",
+            "sv_compact_pages", "sv_compact_pages_workspace_size", "sv_copy_pages", "sv_status_string", "sv_last_error", "sv_abi_version")
 
 
 class BudgetDesc(ctypes.Structure):
@@ -63,6 +68,31 @@ class AppendDesc(ctypes.Structure):
     _fields_ = [("num_reqs", ctypes.c_int32), ("total_max", ctypes.c_int32), ("block", ctypes.c_int32),
                 ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("max_pages_per_req", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("num_reqs", ctypes.c_int32), ("total_max", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("num_axes", ctypes.c_int32), ("section", ctypes.c_int32 * SV_MAX_ROPE_AXES),
+                ("order", ctypes.c_int32), ("pairing", ctypes.c_int32), ("q_stride", ctypes.c_int32),
+                ("k_stride", ctypes.c_int32), ("v_stride", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("max_pages_per_req", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class WindowDesc(ctypes.Structure):
+    _fields_ = [("attn", AttnDesc), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+
+
+class PagesDesc(ctypes.Structure):
+    _fields_ = [("num_reqs", ctypes.c_int32), ("max_pages_per_req", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32)]
+
+
+class CopyDesc(ctypes.Structure):
+    _fields_ = [("max_copies", ctypes.c_int32), ("num_layers", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("layer_stride", ctypes.c_int64)]
 
 
 class SpecVerifyError(RuntimeError):
@@ -118,6 +148,26 @@ def load() -> ctypes.CDLL:
     lib.sv_pack_verify.restype = i32
     lib.sv_append_kv.argtypes = [ctypes.POINTER(AppendDesc), P, P, P, P, P, P, P, P]
     lib.sv_append_kv.restype = i32
+    lib.sv_rope_append.argtypes = [ctypes.POINTER(RopeDesc), P, P, P, P, P, P, P, P, P, P, P, P]
+    lib.sv_rope_append.restype = i32
+    lib.sv_window_attn.argtypes = [ctypes.POINTER(WindowDesc), P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P]
+    lib.sv_window_attn.restype = i32
+    lib.sv_window_attn_workspace_size.argtypes = [ctypes.POINTER(WindowDesc)]
+    lib.sv_window_attn_workspace_size.restype = ctypes.c_size_t
+    lib.sv_fork_pages.argtypes = [ctypes.POINTER(PagesDesc), i32, P, P, P, P, P, P, P]
+    lib.sv_fork_pages.restype = i32
+    lib.sv_reserve_pages.argtypes = [ctypes.POINTER(PagesDesc), P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P]
+    lib.sv_reserve_pages.restype = i32
+    lib.sv_reserve_pages_workspace_size.argtypes = [ctypes.POINTER(PagesDesc)]
+    lib.sv_reserve_pages_workspace_size.restype = ctypes.c_size_t
+    lib.sv_release_pages.argtypes = [ctypes.POINTER(PagesDesc), i32, i32, P, P, P, P]
+    lib.sv_release_pages.restype = i32
+    lib.sv_compact_pages.argtypes = [ctypes.POINTER(PagesDesc), i32, P, P, P, P, P, P, ctypes.c_size_t, P]
+    lib.sv_compact_pages.restype = i32
+    lib.sv_compact_pages_workspace_size.argtypes = [ctypes.POINTER(PagesDesc)]
+    lib.sv_compact_pages_workspace_size.restype = ctypes.c_size_t
+    lib.sv_copy_pages.argtypes = [ctypes.POINTER(CopyDesc), P, P, P, P, P, P, P]
+    lib.sv_copy_pages.restype = i32
     lib.sv_status_string.argtypes = [i32]
     lib.sv_status_string.restype = ctypes.c_char_p
     lib.sv_last_error.argtypes = []
@@ -149,6 +199,17 @@ def _ptr(t) -> Optional[int]:
         return t
     if not t.is_contiguous():
         raise ValueError("tensors passed to libspecverify must be contiguous")
+    return t.data_ptr()
+
+
+def _rows_ptr(t, stride: int, name: str) -> int:
+    """Device pointer of rows [n, heads, d] that lie `stride` elements apart (0: dense)."""
+    if isinstance(t, int):
+        return t
+    heads, d = t.shape[1:]
+    want = stride or heads * d
+    if (t.shape[0] > 1 and t.stride(0) != want) or (heads > 1 and t.stride(1) != d) or t.stride(2) != 1:
+        raise ValueError(f"{name}: strides {tuple(t.stride())} are not those of rows {want} elements apart")
     return t.data_ptr()
 
 
@@ -349,4 +410,121 @@ def draft_stats(desc: DraftStatsDesc, draft_logits, stats, conf=None, ws=None, s
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
     st = load().sv_draft_stats(ctypes.byref(desc), _ptr(draft_logits), _ptr(stats), _ptr(conf), _ptr(ws), nbytes,
                                _stream(stream))
+    _check(st)
+
+
+# ------------------------------------------------------------------------------------
+# sv_rope_append
+# ------------------------------------------------------------------------------------
+def rope_desc(R: int, total_max: int, Hq: int, Hkv: int, d: int, sections: Sequence[int], page_size: int,
+              max_pages_per_req: int, num_pages: int, dtype: int, order: int = SV_ROPE_BLOCKS,
+              pairing: int = SV_ROPE_HALVES, rot_dim: int = 0, q_stride: int = 0, k_stride: int = 0,
+              v_stride: int = 0, scale: float = 1.0) -> RopeDesc:
+    """sections: rotated pairs of each position axis; rot_dim 0 = twice their sum. A factor of 0
+    is the library's default of 1."""
+    if not 1 <= len(sections) <= SV_MAX_ROPE_AXES:
+        raise ValueError(f"{len(sections)} position axes (1 to {SV_MAX_ROPE_AXES})")
+    r = RopeDesc()
+    r.num_reqs, r.total_max, r.num_q_heads, r.num_kv_heads, r.head_dim = R, total_max, Hq, Hkv, d
+    r.rot_dim = rot_dim or 2 * sum(sections)
+    r.num_axes = len(sections)
+    for a, n in enumerate(sections):
+        r.section[a] = n
+    r.order, r.pairing = order, pairing
+    r.q_stride, r.k_stride, r.v_stride = q_stride, k_stride, v_stride
+    r.page_size, r.max_pages_per_req, r.num_pages, r.dtype, r.scale = (page_size, max_pages_per_req, num_pages, dtype,
+                                                                      scale)
+    return r
+
+
+def rope_append(desc: RopeDesc, q, k_new, v_new, positions, inv_freq, page_table, qo_indptr, ctx_lens, q_out,
+                k_cache, v_cache, stream=None):
+    """sv_rope_append: q, k_new, v_new [total_max, heads, d] may be parts of wider rows (desc's strides);
+    inv_freq [rot_dim / 2] float64."""
+    st = load().sv_rope_append(ctypes.byref(desc), _rows_ptr(q, desc.q_stride, "q"),
+                               _rows_ptr(k_new, desc.k_stride, "k_new"), _rows_ptr(v_new, desc.v_stride, "v_new"),
+                               _ptr(positions), _ptr(inv_freq), _ptr(page_table), _ptr(qo_indptr), _ptr(ctx_lens),
+                               _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream(stream))
+    _check(st)
+
+
+# ------------------------------------------------------------------------------------
+# sv_window_attn
+# ------------------------------------------------------------------------------------
+def window_desc(attn: AttnDesc, window: int, sinks: int = 0) -> WindowDesc:
+    w = WindowDesc()
+    w.attn, w.window, w.sinks = attn, window, sinks
+    return w
+
+
+def window_attn_workspace_size(desc: WindowDesc) -> int:
+    return int(load().sv_window_attn_workspace_size(ctypes.byref(desc)))
+
+
+def window_attn(desc: WindowDesc, q, k_cache, v_cache, page_table, qo_indptr, kv_lens, out, lse=None, ws=None,
+                stream=None):
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    st = load().sv_window_attn(ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
+                               _ptr(qo_indptr), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(ws), nbytes,
+                               _stream(stream))
+    _check(st)
+
+
+# ------------------------------------------------------------------------------------
+# sv_fork_pages, sv_reserve_pages, sv_release_pages, sv_compact_pages, sv_copy_pages
+# ------------------------------------------------------------------------------------
+def pages_desc(R: int, max_pages_per_req: int, num_pages: int, page_size: int) -> PagesDesc:
+    d = PagesDesc()
+    d.num_reqs, d.max_pages_per_req, d.num_pages, d.page_size = R, max_pages_per_req, num_pages, page_size
+    return d
+
+
+def fork_pages(desc: PagesDesc, rows_in: int, table_in, lens_in, parent, table_out, lens_out, ref, stream=None):
+    st = load().sv_fork_pages(ctypes.byref(desc), rows_in, _ptr(table_in), _ptr(lens_in), _ptr(parent),
+                              _ptr(table_out), _ptr(lens_out), _ptr(ref), _stream(stream))
+    _check(st)
+
+
+def reserve_pages_workspace_size(desc: PagesDesc) -> int:
+    return int(load().sv_reserve_pages_workspace_size(ctypes.byref(desc)))
+
+
+def reserve_pages(desc: PagesDesc, page_table, ref, ctx_lens, new_lens, copy_src, copy_dst, copy_tokens, info,
+                  ws=None, stream=None):
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    st = load().sv_reserve_pages(ctypes.byref(desc), _ptr(page_table), _ptr(ref), _ptr(ctx_lens), _ptr(new_lens),
+                                 _ptr(copy_src), _ptr(copy_dst), _ptr(copy_tokens), _ptr(info), _ptr(ws), nbytes,
+                                 _stream(stream))
+    _check(st)
+
+
+def release_pages(desc: PagesDesc, page_table, ref, lens, window: int = 0, sinks: int = 0, stream=None):
+    st = load().sv_release_pages(ctypes.byref(desc), window, sinks, _ptr(page_table), _ptr(ref), _ptr(lens),
+                                 _stream(stream))
+    _check(st)
+
+
+def compact_pages_workspace_size(desc: PagesDesc) -> int:
+    return int(load().sv_compact_pages_workspace_size(ctypes.byref(desc)))
+
+
+def compact_pages(desc: PagesDesc, max_moves: int, page_table, ref, move_src, move_dst, info, ws=None, stream=None):
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    st = load().sv_compact_pages(ctypes.byref(desc), max_moves, _ptr(page_table), _ptr(ref), _ptr(move_src),
+                                 _ptr(move_dst), _ptr(info), _ptr(ws), nbytes, _stream(stream))
+    _check(st)
+
+
+def copy_desc(max_copies: int, layers: int, Hkv: int, d: int, page_size: int, num_pages: int, dtype: int,
+              layer_stride: int = 0) -> CopyDesc:
+    c = CopyDesc()
+    (c.max_copies, c.num_layers, c.num_kv_heads, c.head_dim, c.page_size, c.num_pages, c.dtype,
+     c.layer_stride) = max_copies, layers, Hkv, d, page_size, num_pages, dtype, layer_stride
+    return c
+
+
+def copy_pages(desc: CopyDesc, src, dst, count, k_cache, v_cache, tokens=None, stream=None):
+    """sv_copy_pages: count is a device tensor of one int32 (reserve_pages: info[2:3], compact_pages: info[:1])."""
+    st = load().sv_copy_pages(ctypes.byref(desc), _ptr(src), _ptr(dst), _ptr(tokens), _ptr(count), _ptr(k_cache),
+                              _ptr(v_cache), _stream(stream))
     _check(st)

@@ -1,0 +1,243 @@
+// Rotary positions on several axes, and the append of the rotated keys and the values to the
+// paged cache (sv_rope_append). A row's angles are the same in all its heads: the first waves
+// compute sine and cosine of each pair once per workgroup into LDS, and the threads then
+// turn 16-byte chunks of the heads. The angle is taken in turns, x * (f / 2 pi) in fp64, and only its
+// fraction goes to fp32, so a far position loses nothing; sine, cosine and the rotation
+// are fp32, with one rounding to the storage type.
+// Bound by the copy of the rows (each read and written once) and, for few rows, by the latency of the
+// dependent steps: the packing, the page, the rows.
+#include <algorithm>
+
+#include "attn_tile.h"
+#include "sv_internal.h"
+
+namespace sv {
+namespace {
+
+struct RopeArgs {
+    const char* q;  // rows q_stride bytes apart
+    const char* k;
+    const char* v;
+    const int32_t* positions;  // [axes, total]
+    const double* inv_freq;    // [pairs]
+    const int32_t* page_table;
+    const int32_t* qo;
+    const int32_t* ctx;
+    char* q_out;
+    char* kc;
+    char* vc;
+    size_t q_stride, k_stride, v_stride;
+    int R, total, Hq, Hkv, d, pairs, axes, cycle, log2P, maxp, num_pages;
+    int section[SV_MAX_ROPE_AXES];
+    float scale;
+    int tasks, tasks_per_head, turns_per_head;  // of a row; of a head of q or k; those that turn pairs
+};
+
+constexpr int kMaxPairs = 512;
+
+// the axis of pair p
+__device__ inline int pair_axis(const RopeArgs& a, int p) {
+    if (a.cycle) {
+        const int x = p % a.axes;
+        return p / a.axes < a.section[x] ? x : 0;
+    }
+    int x = 0, past = a.section[0];
+    while (x + 1 < a.axes && p >= past) past += a.section[++x];
+    return x;
+}
+
+template <typename T> struct Chunk;  // 16 bytes of a row as floats
+template <> struct Chunk<float> {
+    static constexpr int N = 4;
+    static __device__ void get(const uint4& x, float* f) {
+        f[0] = __uint_as_float(x.x), f[1] = __uint_as_float(x.y), f[2] = __uint_as_float(x.z),
+        f[3] = __uint_as_float(x.w);
+    }
+    static __device__ uint4 put(const float* f) {
+        return uint4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+    }
+};
+template <> struct Chunk<uint16_t> {
+    static constexpr int N = 8;
+    static __device__ void get(const uint4& x, float* f) {
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            f[2 * e] = __uint_as_float(w[e] << 16);
+            f[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+        }
+    }
+    static __device__ uint4 put(const float* f) {
+        bf16x8 b;
+#pragma unroll
+        for (int e = 0; e < 8; e++) b[e] = (__bf16)f[e];
+        return __builtin_bit_cast(uint4, b);
+    }
+};
+
+__device__ inline float load1(const float* p) { return *p; }
+__device__ inline float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
+__device__ inline void store1(float* p, float f) { *p = f; }
+__device__ inline void store1(uint16_t* p, float f) { *p = f2bf(f); }
+
+// grid (row, part of the row's tasks). VEC: a task turns the pairs of one chunk (adjacent dims) or of
+// two chunks (dims of either half), or copies a chunk; else it turns one pair, or copies one element.
+template <typename T, bool ADJ, bool VEC>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+    __shared__ float2 cs[kMaxPairs];
+    __shared__ long long s_slot;  // the row's slot in the cache's first kv-head, -1: none
+    __shared__ int s_ok;
+    constexpr int N = VEC ? Chunk<T>::N : 1;
+    const int row = blockIdx.x, tid = threadIdx.x;
+    if (row >= a.qo[a.R]) return;
+    if (tid < 64) {
+        // the request: the last one whose rows start at or before this row, 64 at a time
+        int lo = 0, n = a.R;
+        while (n > 1) {
+            const int step = (n + 63) / 64;
+            const int at = lo + tid * step;
+            const bool before = tid * step < n && a.qo[min(at, a.R)] <= row;
+            const int c = __popcll(__ballot(before));
+            lo += max(c - 1, 0) * step;
+            n = min(step, n - max(c - 1, 0) * step);
+        }
+        if (tid == 0) {
+            const int q0 = a.qo[lo], q1 = a.qo[lo + 1];
+            const bool ok = q0 >= 0 && q0 <= row && row < q1 && q1 <= a.total;
+            long long slot = -1;
+            const int L = a.ctx[lo];
+            if (ok && L >= 0) {
+                const long long s = (long long)L + (row - q0), col = s >> a.log2P;
+                if (col < a.maxp) {
+                    const int pg = a.page_table[(size_t)lo * a.maxp + col];
+                    if (pg >= 0 && pg < a.num_pages)
+                        slot = (((long long)pg * a.Hkv) << a.log2P) + (s & ((1 << a.log2P) - 1));
+                }
+            }
+            s_ok = ok;
+            s_slot = slot;
+        }
+    }
+    for (int p = (tid + 192) & 255; p < a.pairs; p += 256) {
+        const double x = a.positions[(size_t)pair_axis(a, p) * a.total + row] * (a.inv_freq[p] * 0.15915494309189535);
+        float s, c;
+        sincospif((float)(2.0 * (x - rint(x))), &s, &c);
+        cs[p] = float2{c * a.scale, s * a.scale};
+    }
+    __syncthreads();
+    if (!s_ok) return;
+    const long long slot = s_slot;
+    const int heads = a.Hq + a.Hkv, d = a.d, half = a.pairs;
+    for (int t = blockIdx.y * 256 + tid; t < a.tasks; t += gridDim.y * 256) {
+        const bool value = t >= heads * a.tasks_per_head;
+        const int per = value ? d / N : a.tasks_per_head;
+        const int u = value ? t - heads * a.tasks_per_head : t;
+        const int hx = u / per, c = u % per;  // head, task in the head
+        const bool key = !value && hx >= a.Hq;
+        if ((value || key) && slot < 0) continue;
+        const int h = key ? hx - a.Hq : hx;
+        const T* src = (const T*)((value ? a.v + row * a.v_stride : key ? a.k + row * a.k_stride
+                                                                        : a.q + row * a.q_stride)) + (size_t)h * d;
+        T* dst = value || key ? (T*)(value ? a.vc : a.kc) + ((size_t)slot + ((size_t)h << a.log2P)) * d
+                              : (T*)a.q_out + ((size_t)row * a.Hq + h) * d;
+        if (value || c >= a.turns_per_head) {
+            const int at = value ? c * N : 2 * half + (c - a.turns_per_head) * N;
+            if constexpr (VEC) *(uint4*)(dst + at) = *(const uint4*)(src + at);
+            else dst[at] = src[at];
+            continue;
+        }
+        if constexpr (!VEC) {
+            const int i = ADJ ? 2 * c : c, j = ADJ ? 2 * c + 1 : c + half;
+            const float x = load1(src + i), y = load1(src + j);
+            const float2 w = cs[c];
+            store1(dst + i, x * w.x - y * w.y);
+            store1(dst + j, y * w.x + x * w.y);
+        } else if constexpr (ADJ) {
+            float x[N];
+            Chunk<T>::get(*(const uint4*)(src + c * N), x);
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const float2 w = cs[(c * N + e) / 2];
+                const float u0 = x[e] * w.x - x[e + 1] * w.y, u1 = x[e + 1] * w.x + x[e] * w.y;
+                x[e] = u0, x[e + 1] = u1;
+            }
+            *(uint4*)(dst + c * N) = Chunk<T>::put(x);
+        } else {
+            float x[N], y[N];
+            Chunk<T>::get(*(const uint4*)(src + c * N), x);
+            Chunk<T>::get(*(const uint4*)(src + half + c * N), y);
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                const float2 w = cs[c * N + e];
+                const float u0 = x[e] * w.x - y[e] * w.y, u1 = y[e] * w.x + x[e] * w.y;
+                x[e] = u0, y[e] = u1;
+            }
+            *(uint4*)(dst + c * N) = Chunk<T>::put(x);
+            *(uint4*)(dst + half + c * N) = Chunk<T>::put(y);
+        }
+    }
+}
+
+int ilog2i(int x) {
+    int r = 0;
+    while ((1 << r) < x) r++;
+    return r;
+}
+
+}  // namespace
+
+hipError_t launch_rope(const sv_rope_desc& d, const void* q, const void* k_new, const void* v_new,
+                       const int32_t* positions, const double* inv_freq, const int32_t* page_table,
+                       const int32_t* qo_indptr, const int32_t* ctx_lens, void* q_out, void* k_cache, void* v_cache,
+                       hipStream_t stream) {
+    const int esz = d.dtype == SV_F32 ? 4 : 2, N = 16 / esz;
+    RopeArgs a{};
+    a.q = (const char*)q;
+    a.k = (const char*)k_new;
+    a.v = (const char*)v_new;
+    a.positions = positions;
+    a.inv_freq = inv_freq;
+    a.page_table = page_table;
+    a.qo = qo_indptr;
+    a.ctx = ctx_lens;
+    a.q_out = (char*)q_out;
+    a.kc = (char*)k_cache;
+    a.vc = (char*)v_cache;
+    a.q_stride = (size_t)(d.q_stride ? d.q_stride : d.num_q_heads * d.head_dim) * esz;
+    a.k_stride = (size_t)(d.k_stride ? d.k_stride : d.num_kv_heads * d.head_dim) * esz;
+    a.v_stride = (size_t)(d.v_stride ? d.v_stride : d.num_kv_heads * d.head_dim) * esz;
+    a.R = d.num_reqs;
+    a.total = d.total_max;
+    a.Hq = d.num_q_heads;
+    a.Hkv = d.num_kv_heads;
+    a.d = d.head_dim;
+    a.pairs = d.rot_dim / 2;
+    a.axes = d.num_axes;
+    a.cycle = d.order == SV_ROPE_CYCLE;
+    for (int x = 0; x < d.num_axes; x++) a.section[x] = d.section[x];
+    a.log2P = ilog2i(d.page_size);
+    a.maxp = d.max_pages_per_req;
+    a.num_pages = d.num_pages;
+    a.scale = d.scale == 0.0f ? 1.0f : d.scale;
+    const bool adj = d.pairing == SV_ROPE_ADJACENT;
+    // chunks hold whole pairs (adjacent dims), or the same pairs of either half
+    const bool vec = (adj ? d.rot_dim : d.rot_dim / 2) % N == 0;
+    const int n = vec ? N : 1;
+    a.turns_per_head = vec && adj ? d.rot_dim / N : a.pairs / n;
+    a.tasks_per_head = a.turns_per_head + (d.head_dim - d.rot_dim) / n;
+    a.tasks = (d.num_q_heads + d.num_kv_heads) * a.tasks_per_head + d.num_kv_heads * (d.head_dim / n);
+    // a row is divided among workgroups where the rows alone are too few
+    const int parts = std::max(1, std::min((a.tasks + 255) / 256, 2048 / d.total_max));
+    const dim3 grid(d.total_max, parts);
+#define SV_ROPE(T, ADJ, VEC) hipLaunchKernelGGL((rope_kernel<T, ADJ, VEC>), grid, dim3(256), 0, stream, a)
+#define SV_ROPE_TYPE(T) \
+    if (adj) { if (vec) SV_ROPE(T, true, true); else SV_ROPE(T, true, false); } \
+    else { if (vec) SV_ROPE(T, false, true); else SV_ROPE(T, false, false); }
+    if (d.dtype == SV_F32) { SV_ROPE_TYPE(float) }
+    else { SV_ROPE_TYPE(uint16_t) }
+#undef SV_ROPE_TYPE
+#undef SV_ROPE
+    return hipGetLastError();
+}
+
+}  // namespace sv

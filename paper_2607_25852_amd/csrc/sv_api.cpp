@@ -195,6 +195,170 @@ sv_status sv_append_kv(const sv_append_desc* desc, const void* k_new, const void
                     "sv_append_kv");
 }
 
+sv_status sv_rope_append(const sv_rope_desc* desc, const void* q, const void* k_new, const void* v_new,
+                         const int32_t* positions, const double* inv_freq, const int32_t* page_table,
+                         const int32_t* qo_indptr, const int32_t* ctx_lens, void* q_out, void* k_cache, void* v_cache,
+                         void* stream) {
+    CallRange range("sv_rope_append");
+    sv_status st = sv::check_rope(desc);
+    if (st != SV_OK) return st;
+    if (!q || !k_new || !v_new || !positions || !inv_freq || !page_table || !qo_indptr || !ctx_lens || !q_out ||
+        !k_cache || !v_cache)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: a required pointer is NULL");
+    if (!aligned(q, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q_out, 16) || !aligned(k_cache, 16) ||
+        !aligned(v_cache, 16) || !aligned(inv_freq, 8) || !aligned(positions, 4) || !aligned(page_table, 4) ||
+        !aligned(qo_indptr, 4) || !aligned(ctx_lens, 4))
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: rows and caches must be 16-byte aligned, inv_freq 8-byte, int32 "
+                                        "arrays 4-byte aligned");
+    if (q == q_out && desc->q_stride != 0 && desc->q_stride != desc->num_q_heads * desc->head_dim)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: q_out is q, but q_stride %d is not Hq * d", desc->q_stride);
+    if (inject_launch_fault()) return fail(SV_ERR_HIP, "sv_rope_append: injected launch failure");
+    return launched(sv::launch_rope(*desc, q, k_new, v_new, positions, inv_freq, page_table, qo_indptr, ctx_lens, q_out,
+                                    k_cache, v_cache, (hipStream_t)stream),
+                    "sv_rope_append");
+}
+
+size_t sv_window_attn_workspace_size(const sv_window_desc* desc) {
+    if (sv::check_window(desc) != SV_OK) return 0;
+    return sv::window_workspace(*desc);
+}
+
+sv_status sv_window_attn(const sv_window_desc* desc, const void* q, const void* k_cache, const void* v_cache,
+                         const int32_t* page_table, const int32_t* qo_indptr, const int32_t* kv_lens, void* out,
+                         float* lse, void* ws, size_t ws_bytes, void* stream) {
+    CallRange range("sv_window_attn");
+    sv_status st = sv::check_window(desc);
+    if (st != SV_OK) return st;
+    if (!q || !k_cache || !v_cache || !page_table || !qo_indptr || !kv_lens || !out)
+        return fail(SV_ERR_INVALID_ARG, "sv_window_attn: a required pointer is NULL");
+    if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) || !aligned(ws, 16) ||
+        !aligned(page_table, 4) || !aligned(qo_indptr, 4) || !aligned(kv_lens, 4) || !aligned(lse, 4))
+        return fail(SV_ERR_INVALID_ARG,
+                    "sv_window_attn: q, caches, out and ws must be 16-byte aligned, int32/fp32 arrays 4-byte aligned");
+    const size_t need = sv::window_workspace(*desc);
+    if (need && (!ws || ws_bytes < need))
+        return fail(SV_ERR_WORKSPACE, "sv_window_attn: workspace of %zu bytes needed, %zu given", need,
+                    ws ? ws_bytes : (size_t)0);
+    if (inject_launch_fault()) return fail(SV_ERR_HIP, "sv_window_attn: injected launch failure");
+    return launched(sv::launch_window(*desc, q, k_cache, v_cache, page_table, qo_indptr, kv_lens, out, lse, ws,
+                                      (hipStream_t)stream),
+                    "sv_window_attn");
+}
+
+sv_status sv_fork_pages(const sv_pages_desc* desc, int32_t rows_in, const int32_t* table_in, const int32_t* lens_in,
+                        const int32_t* parent, int32_t* table_out, int32_t* lens_out, int32_t* ref, void* stream) {
+    CallRange range("sv_fork_pages");
+    sv_status st = sv::check_pages("sv_fork_pages", desc);
+    if (st != SV_OK) return st;
+    const sv_pages_desc& d = *desc;
+    if (rows_in < 1 || rows_in > 65535 || (long long)rows_in * d.max_pages_per_req > 0x7FFFFFFFLL)
+        return fail(SV_ERR_INVALID_ARG, "sv_fork_pages: rows_in %d outside [1, 65535], or its table has 2^31 entries",
+                    rows_in);
+    if (!table_in || !lens_in || !parent || !table_out || !lens_out || !ref)
+        return fail(SV_ERR_INVALID_ARG, "sv_fork_pages: a required pointer is NULL");
+    if (!aligned(table_in, 4) || !aligned(lens_in, 4) || !aligned(parent, 4) || !aligned(table_out, 4) ||
+        !aligned(lens_out, 4) || !aligned(ref, 4))
+        return fail(SV_ERR_INVALID_ARG, "sv_fork_pages: arrays must be 4-byte aligned");
+    const uintptr_t in = (uintptr_t)table_in, out = (uintptr_t)table_out;
+    if (in < out + 4ull * d.num_reqs * d.max_pages_per_req && out < in + 4ull * rows_in * d.max_pages_per_req)
+        return fail(SV_ERR_INVALID_ARG, "sv_fork_pages: table_in and table_out overlap");
+    if (inject_launch_fault()) return fail(SV_ERR_HIP, "sv_fork_pages: injected launch failure");
+    return launched(sv::launch_fork(d, rows_in, table_in, lens_in, parent, table_out, lens_out, ref,
+                                    (hipStream_t)stream),
+                    "sv_fork_pages");
+}
+
+namespace {
+sv_status check_reserve(const sv_pages_desc* desc) {
+    const sv_status st = sv::check_pages("sv_reserve_pages", desc);
+    if (st != SV_OK) return st;
+    if (desc->num_reqs > SV_MAX_RESERVE_REQS)
+        return fail(SV_ERR_UNSUPPORTED, "sv_reserve_pages: num_reqs %d above %d", desc->num_reqs, SV_MAX_RESERVE_REQS);
+    return SV_OK;
+}
+}  // namespace
+
+size_t sv_reserve_pages_workspace_size(const sv_pages_desc* desc) {
+    return check_reserve(desc) == SV_OK ? sv::plan_reserve(*desc).ws_bytes : 0;
+}
+
+sv_status sv_reserve_pages(const sv_pages_desc* desc, int32_t* page_table, int32_t* ref, const int32_t* ctx_lens,
+                           const int32_t* new_lens, int32_t* copy_src, int32_t* copy_dst, int32_t* copy_tokens,
+                           int32_t* info, void* ws, size_t ws_bytes, void* stream) {
+    CallRange range("sv_reserve_pages");
+    sv_status st = check_reserve(desc);
+    if (st != SV_OK) return st;
+    if (!page_table || !ref || !ctx_lens || !new_lens || !copy_src || !copy_dst || !copy_tokens || !info)
+        return fail(SV_ERR_INVALID_ARG, "sv_reserve_pages: a required pointer is NULL");
+    if (!aligned(page_table, 4) || !aligned(ref, 4) || !aligned(ctx_lens, 4) || !aligned(new_lens, 4) ||
+        !aligned(copy_src, 4) || !aligned(copy_dst, 4) || !aligned(copy_tokens, 4) || !aligned(info, 4) ||
+        !aligned(ws, 16))
+        return fail(SV_ERR_INVALID_ARG, "sv_reserve_pages: int32 arrays 4-byte aligned, ws 16-byte aligned");
+    const sv::ReservePlan p = sv::plan_reserve(*desc);
+    if (!ws || ws_bytes < p.ws_bytes)
+        return fail(SV_ERR_WORKSPACE, "sv_reserve_pages: workspace of %zu bytes needed, %zu given", p.ws_bytes,
+                    ws ? ws_bytes : (size_t)0);
+    if (inject_launch_fault()) return fail(SV_ERR_HIP, "sv_reserve_pages: injected launch failure");
+    return launched(sv::launch_reserve(*desc, p, page_table, ref, ctx_lens, new_lens, copy_src, copy_dst, copy_tokens,
+                                       info, ws, (hipStream_t)stream),
+                    "sv_reserve_pages");
+}
+
+sv_status sv_release_pages(const sv_pages_desc* desc, int32_t window, int32_t sinks, int32_t* page_table, int32_t* ref,
+                           const int32_t* lens, void* stream) {
+    CallRange range("sv_release_pages");
+    sv_status st = sv::check_pages("sv_release_pages", desc);
+    if (st != SV_OK) return st;
+    if (window < 0 || sinks < 0)
+        return fail(SV_ERR_INVALID_ARG, "sv_release_pages: window %d and sinks %d must be >= 0", window, sinks);
+    if (!page_table || !ref || !lens) return fail(SV_ERR_INVALID_ARG, "sv_release_pages: a required pointer is NULL");
+    if (!aligned(page_table, 4) || !aligned(ref, 4) || !aligned(lens, 4))
+        return fail(SV_ERR_INVALID_ARG, "sv_release_pages: arrays must be 4-byte aligned");
+    if (inject_launch_fault()) return fail(SV_ERR_HIP, "sv_release_pages: injected launch failure");
+    return launched(sv::launch_release(*desc, window, sinks, page_table, ref, lens, (hipStream_t)stream),
+                    "sv_release_pages");
+}
+
+size_t sv_compact_pages_workspace_size(const sv_pages_desc* desc) {
+    return sv::check_pages("sv_compact_pages", desc) == SV_OK ? sv::plan_compact(*desc, 0).ws_bytes : 0;
+}
+
+sv_status sv_compact_pages(const sv_pages_desc* desc, int32_t max_moves, int32_t* page_table, int32_t* ref,
+                           int32_t* move_src, int32_t* move_dst, int32_t* info, void* ws, size_t ws_bytes,
+                           void* stream) {
+    CallRange range("sv_compact_pages");
+    sv_status st = sv::check_pages("sv_compact_pages", desc);
+    if (st != SV_OK) return st;
+    if (max_moves < 0) return fail(SV_ERR_INVALID_ARG, "sv_compact_pages: max_moves %d < 0", max_moves);
+    if (!page_table || !ref || !move_src || !move_dst || !info)
+        return fail(SV_ERR_INVALID_ARG, "sv_compact_pages: a required pointer is NULL");
+    if (!aligned(page_table, 4) || !aligned(ref, 4) || !aligned(move_src, 4) || !aligned(move_dst, 4) ||
+        !aligned(info, 4) || !aligned(ws, 16))
+        return fail(SV_ERR_INVALID_ARG, "sv_compact_pages: int32 arrays 4-byte aligned, ws 16-byte aligned");
+    const sv::CompactPlan p = sv::plan_compact(*desc, max_moves);
+    if (!ws || ws_bytes < p.ws_bytes)
+        return fail(SV_ERR_WORKSPACE, "sv_compact_pages: workspace of %zu bytes needed, %zu given", p.ws_bytes,
+                    ws ? ws_bytes : (size_t)0);
+    if (inject_launch_fault()) return fail(SV_ERR_HIP, "sv_compact_pages: injected launch failure");
+    return launched(sv::launch_compact(*desc, p, page_table, ref, move_src, move_dst, info, ws, (hipStream_t)stream),
+                    "sv_compact_pages");
+}
+
+sv_status sv_copy_pages(const sv_copy_desc* desc, const int32_t* src, const int32_t* dst, const int32_t* tokens,
+                        const int32_t* count, void* k_cache, void* v_cache, void* stream) {
+    CallRange range("sv_copy_pages");
+    sv_status st = sv::check_copy(desc);
+    if (st != SV_OK) return st;
+    if (!src || !dst || !count || !k_cache || !v_cache)
+        return fail(SV_ERR_INVALID_ARG, "sv_copy_pages: a required pointer is NULL");
+    if (!aligned(src, 4) || !aligned(dst, 4) || !aligned(tokens, 4) || !aligned(count, 4) || !aligned(k_cache, 16) ||
+        !aligned(v_cache, 16))
+        return fail(SV_ERR_INVALID_ARG, "sv_copy_pages: caches must be 16-byte aligned, int32 arrays 4-byte aligned");
+    if (inject_launch_fault()) return fail(SV_ERR_HIP, "sv_copy_pages: injected launch failure");
+    return launched(sv::launch_copy(*desc, src, dst, tokens, count, k_cache, v_cache, (hipStream_t)stream),
+                    "sv_copy_pages");
+}
+
 size_t sv_spec_accept_workspace_size(const sv_accept_desc* desc) {
     if (sv::check_accept(desc) != SV_OK) return 0;
     return sv::plan_accept(*desc).total;

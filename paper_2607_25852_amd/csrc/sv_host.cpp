@@ -67,48 +67,48 @@ sv_status check_budget(const sv_budget_desc* d, const float* conf, const int32_t
     return SV_OK;
 }
 
-sv_status check_attn(const sv_attn_desc* d) {
-    if (!d) return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: desc is NULL");
+sv_status check_attn(const sv_attn_desc* d, const char* name) {
+    if (!d) return fail(SV_ERR_INVALID_ARG, "%s: desc is NULL", name);
     if (d->num_reqs < 1 || d->num_reqs > 65535)
-        return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: num_reqs %d outside [1, 65535]", d->num_reqs);
+        return fail(SV_ERR_INVALID_ARG, "%s: num_reqs %d outside [1, 65535]", name, d->num_reqs);
     if (d->max_kv_len > (1 << 22))
-        return fail(SV_ERR_UNSUPPORTED, "sv_verify_attn: max_kv_len %d above 2^22", d->max_kv_len);
+        return fail(SV_ERR_UNSUPPORTED, "%s: max_kv_len %d above 2^22", name, d->max_kv_len);
     if (d->block < 1 || d->block > SV_MAX_BLOCK)
-        return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: block %d outside [1, %d]", d->block, SV_MAX_BLOCK);
-    if (d->total_q_max < 1) return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: total_q_max %d < 1", d->total_q_max);
+        return fail(SV_ERR_INVALID_ARG, "%s: block %d outside [1, %d]", name, d->block, SV_MAX_BLOCK);
+    if (d->total_q_max < 1) return fail(SV_ERR_INVALID_ARG, "%s: total_q_max %d < 1", name, d->total_q_max);
     // the packed batch holds at most block rows per request, and the fp32 path launches one
     // workgroup per (row, head): both products in 64 bits
     if ((long long)d->total_q_max > (long long)d->num_reqs * d->block)
-        return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: total_q_max %d above num_reqs*block = %lld", d->total_q_max,
+        return fail(SV_ERR_INVALID_ARG, "%s: total_q_max %d above num_reqs*block = %lld", name, d->total_q_max,
                     (long long)d->num_reqs * d->block);
     if (d->num_q_heads > 0 && (long long)d->total_q_max * d->num_q_heads > 0x7FFFFFFFLL)
-        return fail(SV_ERR_UNSUPPORTED, "sv_verify_attn: total_q_max*num_q_heads = %lld above 2^31-1",
+        return fail(SV_ERR_UNSUPPORTED, "%s: total_q_max*num_q_heads = %lld above 2^31-1", name,
                     (long long)d->total_q_max * d->num_q_heads);
     if (d->num_q_heads < 1 || d->num_kv_heads < 1 || d->num_q_heads % d->num_kv_heads != 0)
-        return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: num_q_heads %d is not a multiple of num_kv_heads %d",
+        return fail(SV_ERR_INVALID_ARG, "%s: num_q_heads %d is not a multiple of num_kv_heads %d", name,
                     d->num_q_heads, d->num_kv_heads);
     if (!is_pow2(d->page_size) || d->page_size > 4096)
-        return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: page_size %d is not a power of two <= 4096", d->page_size);
+        return fail(SV_ERR_INVALID_ARG, "%s: page_size %d is not a power of two <= 4096", name, d->page_size);
     if (d->max_pages_per_req < 1 || d->num_pages < 1 || d->max_kv_len < 1)
-        return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: max_pages_per_req, num_pages and max_kv_len must be >= 1");
+        return fail(SV_ERR_INVALID_ARG, "%s: max_pages_per_req, num_pages and max_kv_len must be >= 1", name);
     if ((long long)d->max_pages_per_req * d->page_size < d->max_kv_len)
-        return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: max_pages_per_req*page_size < max_kv_len");
+        return fail(SV_ERR_INVALID_ARG, "%s: max_pages_per_req*page_size < max_kv_len", name);
     if (!(d->sm_scale >= 0.0f) || std::isinf(d->sm_scale))
-        return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: sm_scale must be finite and >= 0");
+        return fail(SV_ERR_INVALID_ARG, "%s: sm_scale must be finite and >= 0", name);
     if (d->kv_split < 0 || d->kv_split % 64 != 0)
-        return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: kv_split %d is not a non-negative multiple of 64", d->kv_split);
+        return fail(SV_ERR_INVALID_ARG, "%s: kv_split %d is not a non-negative multiple of 64", name, d->kv_split);
     const int G = d->num_q_heads / d->num_kv_heads;
     if (d->dtype == SV_BF16) {
         if (d->head_dim != 64 && d->head_dim != 128)
-            return fail(SV_ERR_UNSUPPORTED, "sv_verify_attn: bf16 head_dim %d (supported: 64, 128)", d->head_dim);
+            return fail(SV_ERR_UNSUPPORTED, "%s: bf16 head_dim %d (supported: 64, 128)", name, d->head_dim);
         if ((long long)G * d->block > 1024)
-            return fail(SV_ERR_UNSUPPORTED, "sv_verify_attn: group size * block = %lld above 1024", (long long)G * d->block);
+            return fail(SV_ERR_UNSUPPORTED, "%s: group size * block = %lld above 1024", name, (long long)G * d->block);
     } else if (d->dtype == SV_F32) {
         if (d->head_dim < 4 || d->head_dim > 256 || d->head_dim % 4 != 0)
-            return fail(SV_ERR_UNSUPPORTED, "sv_verify_attn: fp32 head_dim %d (supported: multiples of 4 up to 256)",
+            return fail(SV_ERR_UNSUPPORTED, "%s: fp32 head_dim %d (supported: multiples of 4 up to 256)", name,
                         d->head_dim);
     } else {
-        return fail(SV_ERR_INVALID_ARG, "sv_verify_attn: unknown dtype %d", d->dtype);
+        return fail(SV_ERR_INVALID_ARG, "%s: unknown dtype %d", name, d->dtype);
     }
     return SV_OK;
 }
@@ -195,7 +195,135 @@ sv_status check_draft_stats(const sv_draft_stats_desc* d) {
     return SV_OK;
 }
 
+sv_status check_rope(const sv_rope_desc* desc) {
+    if (!desc) return fail(SV_ERR_INVALID_ARG, "sv_rope_append: desc is NULL");
+    const sv_rope_desc& d = *desc;
+    if (d.num_reqs < 1 || d.num_reqs > 65535)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: num_reqs %d outside [1, 65535]", d.num_reqs);
+    if (d.total_max < 1 || d.num_q_heads < 1 || d.num_kv_heads < 1 || d.max_pages_per_req < 1 || d.num_pages < 1)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: total_max, num_q_heads, num_kv_heads, max_pages_per_req and "
+                                        "num_pages must be >= 1");
+    if (!is_pow2(d.page_size) || d.page_size > 4096)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: page_size %d is not a power of two <= 4096", d.page_size);
+    if (d.dtype != SV_F32 && d.dtype != SV_BF16)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: unknown dtype %d", d.dtype);
+    const int vec = d.dtype == SV_F32 ? 4 : 8;  // elements of 16 bytes
+    if (d.head_dim < 1 || d.head_dim > 1024 || d.head_dim % vec != 0)
+        return fail(SV_ERR_UNSUPPORTED, "sv_rope_append: head_dim %d (supported: rows of a multiple of 16 bytes, up to "
+                                        "1024)",
+                    d.head_dim);
+    if (d.rot_dim < 2 || d.rot_dim > d.head_dim || d.rot_dim % 2 != 0)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: rot_dim %d is not even in [2, head_dim]", d.rot_dim);
+    if (d.num_axes < 1 || d.num_axes > SV_MAX_ROPE_AXES)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: num_axes %d outside [1, %d]", d.num_axes, SV_MAX_ROPE_AXES);
+    if (d.order != SV_ROPE_BLOCKS && d.order != SV_ROPE_CYCLE)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: unknown order %d", d.order);
+    if (d.pairing != SV_ROPE_HALVES && d.pairing != SV_ROPE_ADJACENT)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: unknown pairing %d", d.pairing);
+    const int pairs = d.rot_dim / 2;
+    long long sum = 0;
+    for (int x = 0; x < d.num_axes; x++) {
+        if (d.section[x] < 0) return fail(SV_ERR_INVALID_ARG, "sv_rope_append: section[%d] = %d < 0", x, d.section[x]);
+        sum += d.section[x];
+        // every pair that the axis should have must exist: the last is x + num_axes * (section - 1)
+        if (d.order == SV_ROPE_CYCLE && x > 0 && d.section[x] > 0 &&
+            x + (long long)d.num_axes * (d.section[x] - 1) >= pairs)
+            return fail(SV_ERR_INVALID_ARG, "sv_rope_append: section[%d] = %d in turn with %d axes passes rot_dim / 2 = %d",
+                        x, d.section[x], d.num_axes, pairs);
+    }
+    if (sum != pairs)
+        return fail(SV_ERR_INVALID_ARG, "sv_rope_append: the sections sum to %lld, not rot_dim / 2 = %d", sum, pairs);
+    if (!std::isfinite(d.scale)) return fail(SV_ERR_INVALID_ARG, "sv_rope_append: scale must be finite");
+    const long long q_row = (long long)d.num_q_heads * d.head_dim, kv_row = (long long)d.num_kv_heads * d.head_dim;
+    if (q_row > (1 << 24) || kv_row > (1 << 24))
+        return fail(SV_ERR_UNSUPPORTED, "sv_rope_append: a row of %lld elements", std::max(q_row, kv_row));
+    if (d.total_max > (1 << 23) || (long long)d.total_max * std::max(d.num_q_heads, d.num_kv_heads) > 0x7FFFFFFFLL)
+        return fail(SV_ERR_UNSUPPORTED, "sv_rope_append: %d rows exceed one launch", d.total_max);
+    const int strides[3] = {d.q_stride, d.k_stride, d.v_stride};
+    for (int x = 0; x < 3; x++)
+        if (strides[x] != 0 && (strides[x] < (x == 0 ? q_row : kv_row) || strides[x] % vec != 0))
+            return fail(SV_ERR_INVALID_ARG, "sv_rope_append: %c_stride %d is below the row or not a multiple of 16 bytes",
+                        "qkv"[x], strides[x]);
+    return SV_OK;
+}
+
+sv_status check_window(const sv_window_desc* d) {
+    if (!d) return fail(SV_ERR_INVALID_ARG, "sv_window_attn: desc is NULL");
+    const sv_status st = check_attn(&d->attn, "sv_window_attn");
+    if (st != SV_OK) return st;
+    if (d->window < 1) return fail(SV_ERR_INVALID_ARG, "sv_window_attn: window %d < 1", d->window);
+    if (d->sinks < 0) return fail(SV_ERR_INVALID_ARG, "sv_window_attn: sinks %d < 0", d->sinks);
+    return SV_OK;
+}
+
+sv_status check_pages(const char* name, const sv_pages_desc* d) {
+    if (!d) return fail(SV_ERR_INVALID_ARG, "%s: desc is NULL", name);
+    if (d->num_reqs < 1 || d->num_reqs > 65535)
+        return fail(SV_ERR_INVALID_ARG, "%s: num_reqs %d outside [1, 65535]", name, d->num_reqs);
+    if (d->max_pages_per_req < 1 || (long long)d->num_reqs * d->max_pages_per_req > 0x7FFFFFFFLL)
+        return fail(SV_ERR_INVALID_ARG, "%s: max_pages_per_req %d < 1, or the table has 2^31 entries", name,
+                    d->max_pages_per_req);
+    if (d->num_pages < 1 || d->num_pages > (1 << 24))
+        return fail(SV_ERR_INVALID_ARG, "%s: num_pages %d outside [1, 2^24]", name, d->num_pages);
+    if (!is_pow2(d->page_size) || d->page_size > 4096)
+        return fail(SV_ERR_INVALID_ARG, "%s: page_size %d is not a power of two <= 4096", name, d->page_size);
+    return SV_OK;
+}
+
+sv_status check_copy(const sv_copy_desc* desc) {
+    if (!desc) return fail(SV_ERR_INVALID_ARG, "sv_copy_pages: desc is NULL");
+    const sv_copy_desc& d = *desc;
+    if (d.max_copies < 1 || d.num_layers < 1 || d.num_kv_heads < 1 || d.num_pages < 1)
+        return fail(SV_ERR_INVALID_ARG, "sv_copy_pages: max_copies, num_layers, num_kv_heads and num_pages must be >= 1");
+    if (!is_pow2(d.page_size) || d.page_size > 4096)
+        return fail(SV_ERR_INVALID_ARG, "sv_copy_pages: page_size %d is not a power of two <= 4096", d.page_size);
+    if (d.dtype != SV_F32 && d.dtype != SV_BF16)
+        return fail(SV_ERR_INVALID_ARG, "sv_copy_pages: unknown dtype %d", d.dtype);
+    const long long esz = d.dtype == SV_F32 ? 4 : 2;
+    if (d.head_dim < 1 || d.head_dim * esz % 16 != 0 || d.head_dim * esz > (1 << 16))
+        return fail(SV_ERR_UNSUPPORTED, "sv_copy_pages: head_dim %d (the row must be a multiple of 16 bytes)", d.head_dim);
+    const long long row = d.head_dim * esz * d.page_size;  // of a head (below 2^29)
+    if (d.num_kv_heads > (1LL << 30) / row)
+        return fail(SV_ERR_UNSUPPORTED, "sv_copy_pages: a page of %d heads x %lld bytes is above 2^30", d.num_kv_heads, row);
+    if (d.num_layers > (1 << 16) || d.max_copies > (1 << 24) || d.num_pages > (1 << 24))
+        return fail(SV_ERR_UNSUPPORTED, "sv_copy_pages: above 2^16 layers, 2^24 copies or 2^24 pages");
+    const long long dense = row / esz * d.num_kv_heads * d.num_pages;  // elements of a layer
+    if (d.layer_stride != 0 && (d.layer_stride < dense || d.layer_stride * esz % 16 != 0 || d.layer_stride > (1LL << 50)))
+        return fail(SV_ERR_INVALID_ARG, "sv_copy_pages: layer_stride %lld is below a layer's cache (%lld), or not a "
+                                        "multiple of 16 bytes",
+                    (long long)d.layer_stride, dense);
+    return SV_OK;
+}
+
 // ---- workspace layouts ----------------------------------------------------------
+
+ReservePlan plan_reserve(const sv_pages_desc& d) {
+    ReservePlan p{};
+    p.chunks = (d.num_pages + kPageChunkSize - 1) / kPageChunkSize;
+    const size_t n = d.num_pages, R = d.num_reqs;
+    p.writers = 0;
+    p.last = n;
+    p.demand = 2 * n;
+    p.copy_of = 3 * n;
+    p.upto = 4 * n;
+    p.copies = p.upto + R;
+    p.chunk_free = p.copies + R;
+    p.ws_bytes = (p.chunk_free + p.chunks) * sizeof(int32_t);
+    return p;
+}
+
+CompactPlan plan_compact(const sv_pages_desc& d, int max_moves) {
+    CompactPlan p{};
+    p.chunks = (d.num_pages + kPageChunkSize - 1) / kPageChunkSize;
+    p.limit = d.num_pages / 2;
+    if (max_moves > 0) p.limit = std::min(p.limit, max_moves);
+    p.chunk_live = 0;
+    p.move_of = p.chunks;
+    p.ws_bytes = (p.move_of + d.num_pages) * sizeof(int32_t);
+    return p;
+}
+
+size_t window_workspace(const sv_window_desc&) { return 0; }
 
 AttnPlan plan_attn(const sv_attn_desc& d) {
     AttnPlan p{};

@@ -50,7 +50,19 @@ struct AcceptPlan {
     int res_chunks;
     size_t off_cnt, off_stats_t, off_stats_q, off_plan, off_csum, off_tsum, total;  // off_tsum 0: none
 };
+constexpr int kPageChunkSize = 4096;  // pages per workgroup of the page calls
+struct ReservePlan {  // offsets in int32 words
+    int chunks;
+    size_t writers, last, demand, copy_of, upto, copies, chunk_free, ws_bytes;
+};
+struct CompactPlan {
+    int chunks, limit;  // limit: entries of the move list
+    size_t chunk_live, move_of, ws_bytes;
+};
 AttnPlan plan_attn(const sv_attn_desc& d);
+ReservePlan plan_reserve(const sv_pages_desc& d);
+CompactPlan plan_compact(const sv_pages_desc& d, int max_moves);
+size_t window_workspace(const sv_window_desc& d);
 AcceptPlan plan_accept(const sv_accept_desc& d);
 size_t draft_stats_workspace(const sv_draft_stats_desc& d);
 
@@ -61,10 +73,14 @@ const char* last_error();
 bool aligned(const void* p, size_t a);  // NULL counts as aligned
 sv_status check_budget(const sv_budget_desc* d, const float* conf, const int32_t* keep, const int32_t* qo,
                        const int32_t* sel);
-sv_status check_attn(const sv_attn_desc* d);
+sv_status check_attn(const sv_attn_desc* d, const char* name = "sv_verify_attn");
 sv_status check_accept(const sv_accept_desc* d);
 sv_status check_pack(const sv_pack_desc* d);
 sv_status check_append(const sv_append_desc* d);
 sv_status check_draft_stats(const sv_draft_stats_desc* d);
+sv_status check_rope(const sv_rope_desc* d);
+sv_status check_window(const sv_window_desc* d);
+sv_status check_pages(const char* name, const sv_pages_desc* d);
+sv_status check_copy(const sv_copy_desc* d);
 
 }  // namespace sv

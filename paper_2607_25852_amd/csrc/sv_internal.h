@@ -47,6 +47,27 @@ hipError_t launch_draft_stats(const sv_draft_stats_desc& d, const void* logits, 
 hipError_t launch_pack(const sv_pack_desc& d, const int32_t* block_tokens, const int32_t* ctx_lens,
                        const int32_t* qo_indptr, int32_t* tokens, int32_t* positions, int32_t* kv_lens,
                        hipStream_t stream);
+// ---- the paged cache around the round ---------------------------------------------
+hipError_t launch_rope(const sv_rope_desc& d, const void* q, const void* k_new, const void* v_new,
+                       const int32_t* positions, const double* inv_freq, const int32_t* page_table,
+                       const int32_t* qo_indptr, const int32_t* ctx_lens, void* q_out, void* k_cache, void* v_cache,
+                       hipStream_t stream);
+hipError_t launch_window(const sv_window_desc& d, const void* q, const void* k_cache, const void* v_cache,
+                         const int32_t* page_table, const int32_t* qo_indptr, const int32_t* kv_lens, void* out,
+                         float* lse, void* ws, hipStream_t stream);
+hipError_t launch_fork(const sv_pages_desc& d, int rows_in, const int32_t* table_in, const int32_t* lens_in,
+                       const int32_t* parent, int32_t* table_out, int32_t* lens_out, int32_t* ref,
+                       hipStream_t stream);
+hipError_t launch_release(const sv_pages_desc& d, int window, int sinks, int32_t* table, int32_t* ref,
+                          const int32_t* lens, hipStream_t stream);
+hipError_t launch_reserve(const sv_pages_desc& d, const ReservePlan& p, int32_t* table, int32_t* ref,
+                          const int32_t* ctx, const int32_t* new_lens, int32_t* copy_src, int32_t* copy_dst,
+                          int32_t* copy_tokens, int32_t* info, void* ws, hipStream_t stream);
+hipError_t launch_compact(const sv_pages_desc& d, const CompactPlan& p, int32_t* table, int32_t* ref,
+                          int32_t* move_src, int32_t* move_dst, int32_t* info, void* ws, hipStream_t stream);
+hipError_t launch_copy(const sv_copy_desc& d, const int32_t* src, const int32_t* dst, const int32_t* tokens,
+                       const int32_t* count, void* k_cache, void* v_cache, hipStream_t stream);
+
 hipError_t launch_append(const sv_append_desc& d, const void* k_new, const void* v_new, const int32_t* page_table,
                          const int32_t* qo_indptr, const int32_t* ctx_lens, void* k_cache, void* v_cache,
                          hipStream_t stream);
