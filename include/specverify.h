@@ -383,7 +383,7 @@ size_t sv_window_attn_workspace_size(const sv_window_desc* desc);
 
 typedef struct {
     int32_t num_reqs;          /* R in [1, 65535] rows of the page table            */
-    int32_t max_pages_per_req; /* columns of the page table; R * columns < 2^31     */
+    int32_t max_pages_per_req; /* columns of the page table; R * columns <= 2^30    */
     int32_t num_pages;         /* pages in the cache, <= 2^24                       */
     int32_t page_size;         /* P, a power of two in [1, 4096]                    */
 } sv_pages_desc;

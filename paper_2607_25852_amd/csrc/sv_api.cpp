@@ -220,7 +220,7 @@ sv_status sv_rope_append(const sv_rope_desc* desc, const void* q, const void* k_
 
 size_t sv_window_attn_workspace_size(const sv_window_desc* desc) {
     if (sv::check_window(desc) != SV_OK) return 0;
-    return sv::window_workspace(*desc);
+    return sv::plan_window(*desc).ws_bytes;
 }
 
 sv_status sv_window_attn(const sv_window_desc* desc, const void* q, const void* k_cache, const void* v_cache,
@@ -235,12 +235,13 @@ sv_status sv_window_attn(const sv_window_desc* desc, const void* q, const void* 
         !aligned(page_table, 4) || !aligned(qo_indptr, 4) || !aligned(kv_lens, 4) || !aligned(lse, 4))
         return fail(SV_ERR_INVALID_ARG,
                     "sv_window_attn: q, caches, out and ws must be 16-byte aligned, int32/fp32 arrays 4-byte aligned");
-    const size_t need = sv::window_workspace(*desc);
+    const sv::WindowPlan p = sv::plan_window(*desc);
+    const size_t need = p.ws_bytes;
     if (need && (!ws || ws_bytes < need))
         return fail(SV_ERR_WORKSPACE, "sv_window_attn: workspace of %zu bytes needed, %zu given", need,
                     ws ? ws_bytes : (size_t)0);
     if (inject_launch_fault()) return fail(SV_ERR_HIP, "sv_window_attn: injected launch failure");
-    return launched(sv::launch_window(*desc, q, k_cache, v_cache, page_table, qo_indptr, kv_lens, out, lse, ws,
+    return launched(sv::launch_window(*desc, p, q, k_cache, v_cache, page_table, qo_indptr, kv_lens, out, lse, ws,
                                       (hipStream_t)stream),
                     "sv_window_attn");
 }
@@ -251,8 +252,8 @@ sv_status sv_fork_pages(const sv_pages_desc* desc, int32_t rows_in, const int32_
     sv_status st = sv::check_pages("sv_fork_pages", desc);
     if (st != SV_OK) return st;
     const sv_pages_desc& d = *desc;
-    if (rows_in < 1 || rows_in > 65535 || (long long)rows_in * d.max_pages_per_req > 0x7FFFFFFFLL)
-        return fail(SV_ERR_INVALID_ARG, "sv_fork_pages: rows_in %d outside [1, 65535], or its table has 2^31 entries",
+    if (rows_in < 1 || rows_in > 65535 || (long long)rows_in * d.max_pages_per_req > (1 << 30))
+        return fail(SV_ERR_INVALID_ARG, "sv_fork_pages: rows_in %d outside [1, 65535], or its table is above 2^30 entries",
                     rows_in);
     if (!table_in || !lens_in || !parent || !table_out || !lens_out || !ref)
         return fail(SV_ERR_INVALID_ARG, "sv_fork_pages: a required pointer is NULL");

@@ -253,6 +253,13 @@ sv_status check_window(const sv_window_desc* d) {
     if (st != SV_OK) return st;
     if (d->window < 1) return fail(SV_ERR_INVALID_ARG, "sv_window_attn: window %d < 1", d->window);
     if (d->sinks < 0) return fail(SV_ERR_INVALID_ARG, "sv_window_attn: sinks %d < 0", d->sinks);
+    // one flat grid of 256-thread workgroups: its work items must fit the 32-bit dispatch size
+    const WindowPlan p = plan_window(*d);
+    const long long groups = d->attn.dtype == SV_F32
+                                 ? (long long)d->attn.total_q_max * d->attn.num_q_heads
+                                 : ((long long)d->attn.num_reqs * p.splits * d->attn.num_kv_heads + 7) * p.row_blocks;
+    if (groups > (1 << 24) - 1)
+        return fail(SV_ERR_UNSUPPORTED, "sv_window_attn: %lld work items exceed one launch", groups);
     return SV_OK;
 }
 
@@ -260,8 +267,8 @@ sv_status check_pages(const char* name, const sv_pages_desc* d) {
     if (!d) return fail(SV_ERR_INVALID_ARG, "%s: desc is NULL", name);
     if (d->num_reqs < 1 || d->num_reqs > 65535)
         return fail(SV_ERR_INVALID_ARG, "%s: num_reqs %d outside [1, 65535]", name, d->num_reqs);
-    if (d->max_pages_per_req < 1 || (long long)d->num_reqs * d->max_pages_per_req > 0x7FFFFFFFLL)
-        return fail(SV_ERR_INVALID_ARG, "%s: max_pages_per_req %d < 1, or the table has 2^31 entries", name,
+    if (d->max_pages_per_req < 1 || (long long)d->num_reqs * d->max_pages_per_req > (1 << 30))
+        return fail(SV_ERR_INVALID_ARG, "%s: max_pages_per_req %d < 1, or the table is above 2^30 entries", name,
                     d->max_pages_per_req);
     if (d->num_pages < 1 || d->num_pages > (1 << 24))
         return fail(SV_ERR_INVALID_ARG, "%s: num_pages %d outside [1, 2^24]", name, d->num_pages);
@@ -323,7 +330,36 @@ CompactPlan plan_compact(const sv_pages_desc& d, int max_moves) {
     return p;
 }
 
-size_t window_workspace(const sv_window_desc&) { return 0; }
+WindowPlan plan_window(const sv_window_desc& w) {
+    const sv_attn_desc& d = w.attn;
+    WindowPlan p{};
+    const long long rows = (long long)(d.num_q_heads / d.num_kv_heads) * d.block;
+    p.splits = 1;
+    p.split_tiles = 0x7FFFFFFF;
+    if (d.dtype == SV_F32) return p;
+    // four waves: (32-row group, 32-key part of a tile)
+    p.row_groups = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    p.tile = 32 * (4 / p.row_groups);
+    p.row_blocks = (int)((rows + 32 * p.row_groups - 1) / (32 * p.row_groups));
+    // the longest list: the first tokens' tiles, and the window's with the other rows', which may start
+    // inside a tile
+    const long long span = std::min<long long>(d.max_kv_len, (long long)w.window + d.block - 1);
+    const long long head = std::min<long long>(d.max_kv_len, w.sinks);
+    const long long tiles = std::min((d.max_kv_len + p.tile - 1LL) / p.tile,
+                                     (head + p.tile - 1) / p.tile + (span + p.tile - 2) / p.tile + 1);
+    const long long units = (long long)d.num_reqs * d.num_kv_heads * p.row_blocks;
+    long long per = tiles;
+    if (d.kv_split > 0) per = std::max<long long>(1, d.kv_split / p.tile);
+    else if (units < 512) per = std::max<long long>((256 + p.tile - 1) / p.tile, (tiles * units + 511) / 512);
+    p.split_tiles = (int)std::min(per, tiles);
+    p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
+    if (p.splits > 1) {
+        const size_t n = (size_t)p.splits * d.total_q_max * d.num_q_heads;
+        p.part_o_bytes = n * d.head_dim * sizeof(float);
+        p.ws_bytes = p.part_o_bytes + n * sizeof(float);
+    }
+    return p;
+}
 
 AttnPlan plan_attn(const sv_attn_desc& d) {
     AttnPlan p{};

@@ -59,10 +59,17 @@ struct CompactPlan {
     int chunks, limit;  // limit: entries of the move list
     size_t chunk_live, move_of, ws_bytes;
 };
+struct WindowPlan {
+    int row_groups;   // 32-row groups per workgroup (bf16): 1, 2 or 4
+    int tile;         // keys per tile
+    int row_blocks;   // row blocks of row_groups * 32 rows per (request, kv-head)
+    int splits, split_tiles;  // splits of every key list, tiles of each
+    size_t part_o_bytes, ws_bytes;
+};
 AttnPlan plan_attn(const sv_attn_desc& d);
+WindowPlan plan_window(const sv_window_desc& d);
 ReservePlan plan_reserve(const sv_pages_desc& d);
 CompactPlan plan_compact(const sv_pages_desc& d, int max_moves);
-size_t window_workspace(const sv_window_desc& d);
 AcceptPlan plan_accept(const sv_accept_desc& d);
 size_t draft_stats_workspace(const sv_draft_stats_desc& d);
 

@@ -52,9 +52,9 @@ hipError_t launch_rope(const sv_rope_desc& d, const void* q, const void* k_new, 
                        const int32_t* positions, const double* inv_freq, const int32_t* page_table,
                        const int32_t* qo_indptr, const int32_t* ctx_lens, void* q_out, void* k_cache, void* v_cache,
                        hipStream_t stream);
-hipError_t launch_window(const sv_window_desc& d, const void* q, const void* k_cache, const void* v_cache,
-                         const int32_t* page_table, const int32_t* qo_indptr, const int32_t* kv_lens, void* out,
-                         float* lse, void* ws, hipStream_t stream);
+hipError_t launch_window(const sv_window_desc& d, const WindowPlan& plan, const void* q, const void* k_cache,
+                         const void* v_cache, const int32_t* page_table, const int32_t* qo_indptr,
+                         const int32_t* kv_lens, void* out, float* lse, void* ws, hipStream_t stream);
 hipError_t launch_fork(const sv_pages_desc& d, int rows_in, const int32_t* table_in, const int32_t* lens_in,
                        const int32_t* parent, int32_t* table_out, int32_t* lens_out, int32_t* ref,
                        hipStream_t stream);

@@ -88,7 +88,9 @@ WINDOW = dict(R=4, total_q_max=64, block=16, Hq=32, Hkv=8, d=128, page_size=64, 
 @pytest.mark.parametrize("kw,window,sinks,status,msg", [
     ({}, 0, 0, INVALID, "window"), ({}, -5, 0, INVALID, "window"), ({}, 1, -1, INVALID, "sinks"),
     (dict(Hq=30), 1, 0, INVALID, "multiple"), (dict(d=96), 1, 0, UNSUPPORTED, "head_dim"), (dict(block=17), 1, 0, INVALID, "block"),
-    (dict(total_q_max=65), 1, 0, INVALID, "num_reqs*block"), (dict(kv_split=63), 1, 0, INVALID, "kv_split")])
+    (dict(total_q_max=65), 1, 0, INVALID, "num_reqs*block"),
+    (dict(R=65535, kv_split=64, max_kv_len=8192), 1 << 20, 0, UNSUPPORTED, "one launch"),
+    (dict(R=65535, total_q_max=1 << 19, dtype=B.SV_F32), 1, 0, UNSUPPORTED, "one launch"), (dict(kv_split=63), 1, 0, INVALID, "kv_split")])
 def test_window_descriptor(lib, kw, window, sinks, status, msg):
     d = B.window_desc(B.attn_desc(**{**WINDOW, **kw}), window, sinks)
     assert lib.sv_window_attn(ctypes.byref(d), *[fake(i) for i in range(9)], BIG, None) == status
@@ -125,7 +127,7 @@ def page_calls(lib, d):
 
 @pytest.mark.parametrize("kw,msg", [
     (dict(R=0), "num_reqs"), (dict(R=65536), "num_reqs"), (dict(max_pages_per_req=0), "max_pages_per_req"),
-    (dict(max_pages_per_req=1 << 28), "2^31"), (dict(num_pages=0), "num_pages"), (dict(num_pages=(1 << 24) + 1), "num_pages"),
+    (dict(max_pages_per_req=1 << 28), "2^30"), (dict(num_pages=0), "num_pages"), (dict(num_pages=(1 << 24) + 1), "num_pages"),
     (dict(page_size=0), "page_size"), (dict(page_size=24), "page_size"), (dict(page_size=8192), "page_size")])
 def test_pages_descriptor(lib, kw, msg):
     d = B.pages_desc(**{**PAGES, **kw})
