@@ -175,26 +175,29 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WindowArgs a) {
 // ---------------------------------------------------------------------------------
 // bf16 MFMA kernel
 // ---------------------------------------------------------------------------------
-// A workgroup of RG * TS waves takes one (request, split, kv-head, row block): up to RG * 32 query rows of
-// the kv-head group (row r: position j = r / G, head r % G) against the split's tiles of TS * 32
-// keys. Wave w has rows 32 (w / TS) .. + 31 and keys 32 (w % TS) .. + 31 of every tile. As in
-// attn.hip, S^T = K Q^T puts the scores of a query row into one lane pair, and P^T is then
-// in the operand layout of O^T = V^T P^T, with V read transposed from LDS. K and V tiles come
-// through the page table into an LDS ring by direct loads while earlier tiles are multiplied;
-// the TS parts of a row are merged at the end.
+// A workgroup of NW waves takes one (request, split, kv-head, row block): up to NW * 32 query rows of the
+// kv-head group (row r: position j = r / G, head r % G) against the split's tiles of 64 keys. Where the rows
+// fill half of the waves or less, two waves share 32 rows and take the halves of every tile
+// (parts = 2), else a wave takes both halves one after the other. As in attn.hip, S^T = K Q^T puts
+// the scores of a query row into one lane pair, and P^T is then in the operand layout of
+// O^T = V^T P^T, with V read transposed from LDS. K and V tiles come through the page table into an LDS
+// ring by direct loads while earlier tiles are multiplied; the parts of a row are merged at the end.
 constexpr int kPageSlots = 1024;  // page ids staged at a time
 
-template <int HD, int RG, int TS, int NBUF>
+// How a tile's addresses are found: one page holds the whole tile, one page holds each 1 KB segment of
+// it, or every lane looks its token's page up.
+enum class Pages { kTile, kSegment, kLane };
+
+template <int HD, int NW, int NBUF>
 struct WindowLds {
-    static constexpr int TT = 32 * TS;
     union {
         struct {
-            uint16_t k[NBUF][TT * HD];  // [buffer][token * HD + d], swizzled (attn_tile.h)
-            uint16_t v[NBUF][TT * HD];
+            uint16_t k[NBUF][kTile * HD];  // [buffer][token * HD + d], swizzled (attn_tile.h)
+            uint16_t v[NBUF][kTile * HD];
         };
-        float park[TS == 1 ? 1 : RG * TS * HD * 32];  // the waves' partial outputs
+        float park[NW * HD * 16];  // half of the waves' partial outputs
     };
-    float ml[RG * TS][2][64];
+    float ml[NW][2][64];
     int32_t pid[kPageSlots];
     int32_t holes;  // a page that the list needs is missing
     int32_t dirty;  // a value that only some rows see was not finite
@@ -203,13 +206,13 @@ struct WindowLds {
 // the rows of a row block one by one (rare: see `dirty`)
 template <int HD>
 __device__ __noinline__ void redo_rows(WindowArgs a, int i, int h, int sp, int row0, int M, int q0, int L,
-                                       KeyList list, int TT, int t0, int t1) {
+                                       KeyList list, int t0, int t1) {
     const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
     for (int r = threadIdx.x >> 6; r < M; r += waves) {
         const int rr = row0 + r, jq = rr / a.G, head = h * a.G + rr % a.G;
         const size_t orow = (size_t)(q0 + jq) * a.Hq + head;
         float o[4], m, l;
-        wave_row<uint16_t>(a, (const uint16_t*)a.q + orow * HD, a.page_table + (size_t)i * a.maxp, h, L + jq, list, TT,
+        wave_row<uint16_t>(a, (const uint16_t*)a.q + orow * HD, a.page_table + (size_t)i * a.maxp, h, L + jq, list, kTile,
                            t0, t1, 1, m, l, o);
         const float inv = l == 0.0f ? 0.0f : 1.0f / l, lse = l == 0.0f ? -INFINITY : m + logf(l);
         const bool whole = t1 - t0 == list.nt;
@@ -225,19 +228,29 @@ __device__ __noinline__ void redo_rows(WindowArgs a, int i, int h, int sp, int r
     }
 }
 
-// LANE: pages below a 1 KB segment of a tile, every lane looks its token's page up
-template <int HD, int RG, int TS, int NBUF, bool LANE>
-__global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs a) {
-    constexpr int NW = RG * TS, TT = 32 * TS;
+// wait until at most min(newer, MAX) tiles of IPW loads each are outstanding
+template <int MAX, int IPW>
+__device__ inline void wait_tiles(int newer) {
+    if constexpr (MAX == 0) {
+        wait_vm<0>();
+    } else {
+        if (newer >= MAX) wait_vm<MAX * IPW>();
+        else wait_tiles<MAX - 1, IPW>(newer);
+    }
+}
+
+template <int HD, int NW, int NBUF, Pages PM>
+__global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
     constexpr int CPR = HD / 8;             // 16-byte chunks per token row
     constexpr int TPS = 1024 / (HD * 2);    // tokens per 1 KB DMA segment
-    constexpr int NSEG = TT / TPS;          // segments per tensor per tile
+    constexpr int NSEG = kTile / TPS;       // segments per tensor per tile
     constexpr int IPW = 2 * NSEG / NW;      // DMA instructions per wave per tile
-    static_assert(IPW * NW == 2 * NSEG && IPW >= 1 && (NSEG % IPW) == 0, "DMA split: a wave moves one tensor");
+    static_assert(IPW * NW == 2 * NSEG && (NSEG % IPW) == 0, "DMA split: a wave moves one tensor");
     constexpr int KK = HD / 16;             // MFMA k-steps over the head dim
     constexpr int DT = HD / 32;             // output d-tiles
-    constexpr int PF = NBUF - 1;            // prefetch distance in tiles
-    __shared__ __attribute__((aligned(16))) WindowLds<HD, RG, TS, NBUF> lds;
+    constexpr int log2T64 = 6;
+    static_assert(kTile == 1 << log2T64, "tile");
+    __shared__ __attribute__((aligned(16))) WindowLds<HD, NW, NBUF> lds;
 
     // neighbouring workgroups go to the XCDs in turn: each takes a run of (request, split, kv-head)s, whose heads
     // share pages, and the row blocks of one follow each other
@@ -249,26 +262,25 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
     if (ux >= a.per_xcd || unit >= (unsigned)a.R * (unsigned)a.splits * (unsigned)a.Hkv) return;
     const int h = scalar(unit % (unsigned)a.Hkv), is = scalar(unit / (unsigned)a.Hkv);
     const int sp = scalar((unsigned)is % (unsigned)a.splits), i = scalar((unsigned)is / (unsigned)a.splits);
-    const int row0 = rb * RG * 32;
+    const int row0 = rb * NW * 32;
     int q0, k_i, kv_len;
     if (!load_request(a, i, q0, k_i, kv_len)) return;
-    const int M = min(a.G * k_i - row0, RG * 32);
+    const int M = min(a.G * k_i - row0, NW * 32);
     if (M <= 0) return;
     const int L = kv_len - k_i, last = kv_len - 1;  // the first and the last row's position
-    const KeyList list = key_list(a.window, a.sinks, TT, L, k_i);
+    const KeyList list = key_list(a.window, a.sinks, kTile, L, k_i);
     const int t0 = sp * a.split_tiles, t1 = min(list.nt, t0 + a.split_tiles);
     if (t0 >= t1) return;
 
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t* __restrict__ pt = a.page_table + (size_t)i * a.maxp;
-    const int log2S = a.log2P < 31 - __builtin_clz(TT) ? a.log2P : 31 - __builtin_clz(TT);  // tokens per slot
-    const int log2T = 31 - __builtin_clz(TT) - log2S;                                      // slots per tile
+    const int log2S = min(a.log2P, log2T64), log2T = log2T64 - log2S;  // tokens per page slot, slots per tile
     const int chunk_tiles = kPageSlots >> log2T;
     // page ids of tiles c0 .. c1-1 into LDS; a missing page is flagged where a row sees the slot
     auto stage = [&](int c0, int c1) {
         bool hole = false;
         for (int e = tid; e < (c1 - c0) << log2T; e += NW * 64) {
-            const int s = (list_tile(list, c0 + (e >> log2T)) * TT) + ((e & ((1 << log2T) - 1)) << log2S);
+            const int s = list_tile(list, c0 + (e >> log2T)) * kTile + ((e & ((1 << log2T) - 1)) << log2S);
             const int col = s >> a.log2P, pg = col < a.maxp ? pt[col] : -1;
             const bool ok = pg >= 0 && pg < a.num_pages;
             hole |= !ok && s <= last && (s < a.sinks || s + (1 << log2S) > L - a.window + 1);
@@ -278,7 +290,8 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
     };
     if (tid == 0) lds.holes = lds.dirty = 0;
 
-    const int rg = w / TS, th = w % TS;
+    const int parts = M <= NW * 16 ? 2 : 1;
+    const int rg = parts == 2 ? w >> 1 : w, th = parts == 2 ? w & 1 : 0;
     const int r = rg * 32 + (lane & 31), half = lane >> 5;
     const bool row_ok = r < M;
     const int rr = row0 + (row_ok ? r : 0);  // row within the request's kv-head group
@@ -295,7 +308,7 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
 #pragma unroll
             for (int t = 0; t < DT; t++) {
                 const int dd = 32 * t + 16 * (g & 1) + 4 * (jl & 3);
-                vofs[qh][t] = th * 32 * HD + tl * HD + (((dd >> 3) ^ (swz(tl) & (CPR - 1))) << 3) + (dd & 7);
+                vofs[qh][t] = tl * HD + (((dd >> 3) ^ (swz(tl) & (CPR - 1))) << 3) + (dd & 7);
             }
         }
     }
@@ -315,65 +328,82 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
 
     // DMA: wave w moves segments w*IPW .. +IPW-1 of the 2*NSEG of a tile (K first). Lane l of a segment moves
     // position l % CPR of token row seg*TPS + l/CPR, fetching chunk (l % CPR) ^ swz(token). A missing
-    // page, or a segment that no row sees, reads page 0 (which exists); such tokens are masked
-    // out of the scores and zeroed in V.
-    uint32_t voff[IPW];
-    int tk[IPW], sg[IPW];
+    // page reads page 0 (which exists); tokens that no row sees are masked out of the scores and
+    // zeroed in V, whatever was read.
+    const int seg0 = (w * IPW) % NSEG, my_tensor = (w * IPW) / NSEG;
+    uint32_t voff[IPW];  // bytes from the tile (kTile) or the segment
+    int tk[IPW];
 #pragma unroll
     for (int k = 0; k < IPW; k++) {
-        const int seg = (w * IPW + k) % NSEG;
-        const int t = seg * TPS + lane / CPR;
-        tk[k] = t;
-        sg[k] = __builtin_amdgcn_readfirstlane(seg * TPS);
-        voff[k] = (uint32_t)((lane / CPR) * HD + (((lane % CPR) ^ (swz(t) & (CPR - 1))) << 3)) * 2u;
+        tk[k] = (seg0 + k) * TPS + lane / CPR;
+        voff[k] = (uint32_t)((PM == Pages::kTile ? tk[k] : lane / CPR) * HD +
+                             (((lane % CPR) ^ (swz(tk[k]) & (CPR - 1))) << 3)) * 2u;
     }
-    const int my_tensor = __builtin_amdgcn_readfirstlane((w * IPW) / NSEG);
-    const uint16_t* cbase = (const uint16_t*)(my_tensor ? a.vc : a.kc);
-    const uint32_t my_ring = (uint32_t)(uintptr_t)(my_tensor ? &lds.v[0][0] : &lds.k[0][0]) +
-                             (uint32_t)__builtin_amdgcn_readfirstlane(((w * IPW) % NSEG) * 1024);
+    const char* cbase = (const char*)(my_tensor ? a.vc : a.kc);
+    const uint32_t my_ring = (uint32_t)(uintptr_t)(my_tensor ? &lds.v[0][0] : &lds.k[0][0]) + (uint32_t)(seg0 * 1024);
     const int pmask = (1 << a.log2P) - 1;
+    const uint64_t page_bytes = ((uint64_t)a.Hkv << a.log2P) * (HD * 2);
+    const uint64_t head_bytes = ((uint64_t)h << a.log2P) * (HD * 2);
     int ibuf = 0;
-    auto issue_tile = [&](int t, int c0) {
-        const int tb = list_tile(list, t) * TT;
-        const uint32_t lbuf = my_ring + (uint32_t)(ibuf * TT * HD * 2);
-        ibuf = ibuf + 1 == NBUF ? 0 : ibuf + 1;
+    // The page ids of a tile are read from LDS one tile before its copies are issued: lane k has that of segment
+    // k (kLane: every lane has its tokens'), so the look-up's latency is off the path.
+    constexpr int NPG = PM == Pages::kLane ? IPW : 1;
+    int pgv[NPG];
+    auto find_pages = [&](int t, int c0) {
         const int32_t* ids = lds.pid + ((t - c0) << log2T);
+        if constexpr (PM == Pages::kLane) {
 #pragma unroll
-        for (int k = 0; k < IPW; k++) {
-            if constexpr (LANE) {
-                const int tok = tb + tk[k], pg = ids[tk[k] >> log2S];
-                const uint16_t* src = cbase;
-                if (pg >= 0)
-                    src += ((((size_t)pg * a.Hkv + h) << a.log2P) + (size_t)(tok & pmask)) * HD +
-                           (voff[k] / 2 - (lane / CPR) * HD);
-                dma16(src, lbuf + 1024 * k);
-            } else {
-                const int tok = tb + sg[k], pg = max(__builtin_amdgcn_readfirstlane(ids[sg[k] >> log2S]), 0);
-                dma16s(voff[k], cbase + ((((size_t)pg * a.Hkv + h) << a.log2P) + (size_t)(tok & pmask)) * HD,
-                       lbuf + 1024 * k);
+            for (int k = 0; k < IPW; k++) pgv[k] = ids[tk[k] >> log2S];
+        } else if constexpr (PM == Pages::kSegment) {
+            pgv[0] = ids[((seg0 + (lane & (IPW - 1))) * TPS) >> log2S];
+        } else {
+            pgv[0] = ids[0];
+        }
+    };
+    auto issue_tile = [&](int t) {
+        const int tb = list_tile(list, t) * kTile;
+        const uint32_t lbuf = my_ring + (uint32_t)(ibuf * kTile * HD * 2);
+        ibuf = ibuf + 1 == NBUF ? 0 : ibuf + 1;
+        if constexpr (PM == Pages::kTile) {
+            const unsigned pg = max(__builtin_amdgcn_readfirstlane(pgv[0]), 0);
+            const char* base = cbase + pg * page_bytes + head_bytes + (uint32_t)(tb & pmask) * (HD * 2);
+#pragma unroll
+            for (int k = 0; k < IPW; k++) dma16s(voff[k], base, lbuf + 1024 * k);
+        } else {
+#pragma unroll
+            for (int k = 0; k < IPW; k++) {
+                if constexpr (PM == Pages::kLane) {
+                    const char* src = cbase;
+                    if (pgv[k] >= 0)
+                        src += (unsigned)pgv[k] * page_bytes + head_bytes + (uint32_t)((tb + tk[k]) & pmask) * (HD * 2) +
+                               (voff[k] - (uint32_t)(lane / CPR) * (HD * 2));
+                    dma16(src, lbuf + 1024 * k);
+                } else {
+                    const unsigned pg = max(__builtin_amdgcn_readlane(pgv[0], k), 0);
+                    dma16s(voff[k], cbase + pg * page_bytes + head_bytes +
+                                        (uint32_t)((tb + (seg0 + k) * TPS) & pmask) * (HD * 2), lbuf + 1024 * k);
+                }
             }
         }
     };
 
     // what a tile at token tb needs: 0 nothing (every row sees all of it), 1 the mask, 2 mask and page look-up
+    bool holes = false;
     auto tile_edge = [&](int tb) {
-        if (lds.holes) return 2;
-        return tb + TT - 1 <= L && (tb + TT <= a.sinks || tb > last - a.window) ? 0 : 1;
+        return holes ? 2 : (tb + kTile - 1 <= L) & ((tb + kTile <= a.sinks) | (tb > last - a.window)) ? 0 : 1;
     };
     // before the barrier that publishes an edge tile: the lanes that copied V rows which no row sees zero them (P
     // is 0 there, but 0 * NaN is not), and rows that only some see are zeroed if they are not finite: the
     // row block is then done again row by row
-    auto clean_tile = [&](int t, int c0, int buf) {
-        const int tb = list_tile(list, t) * TT;
-        const int edge = tile_edge(tb);
-        if (edge == 0 || my_tensor == 0) return;
+    auto clean_tile = [&](int t, int c0, int buf, int edge) {
+        const int tb = list_tile(list, t) * kTile;
 #pragma unroll
         for (int k = 0; k < IPW; k++) {
             const int s = tb + tk[k];
-            u16x8* at = (u16x8*)((char*)lds.v[buf] + ((w * IPW) % NSEG + k) * 1024 + 16 * lane);
-            bool zero = s > last || (s >= a.sinks && s <= L - a.window);
+            u16x8* at = (u16x8*)((char*)lds.v[buf] + (seg0 + k) * 1024 + 16 * lane);
+            bool zero = (s > last) | ((s >= a.sinks) & (s <= L - a.window));
             if (edge == 2) zero |= lds.pid[((t - c0) << log2T) + (tk[k] >> log2S)] < 0;
-            if (!zero && (s > L || (s >= a.sinks && s <= last - a.window))) {
+            if (!zero && ((s > L) | ((s >= a.sinks) & (s <= last - a.window)))) {
                 const u16x8 v = *at;
 #pragma unroll
                 for (int e = 0; e < 8; e++) zero |= (v[e] & 0x7F80) == 0x7F80;
@@ -383,15 +413,14 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
         }
     };
 
-    auto compute_tile = [&](int t, int c0, int buf) {
-        const uint16_t* kt = lds.k[buf];
-        const uint16_t* vt = lds.v[buf];
-        const int tb = list_tile(list, t) * TT;
-        // S^T = K Q^T of this wave's 32 keys in two chains, operands read KPD products ahead
+    const int sw = swz(lane & 31) & (CPR - 1);
+    // 32 keys of a tile, from key 32 sl on
+    auto compute_half = [&](int t, int c0, int buf, int sl, int edge) {
+        const uint16_t* vt = lds.v[buf] + sl * 32 * HD;
+        // S^T = K Q^T in two chains, operands read KPD products ahead
         f32x16 s;
         {
-            const int sw = swz(lane & 31) & (CPR - 1);
-            const uint16_t* krow = kt + (th * 32 + (lane & 31)) * HD;
+            const uint16_t* krow = lds.k[buf] + (sl * 32 + (lane & 31)) * HD;
             constexpr int KPD = 4;
             auto kread = [&](int j) { return __builtin_bit_cast(bf16x8, *(const u16x8*)(krow + (((2 * j + half) ^ sw) << 3))); };
             bf16x8 kb[KPD + 1];
@@ -408,21 +437,20 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
             }
             s = c0a + c1a;
         }
-        // register e holds key tb + 32 th + 4 half + x, x = 8 (e / 4) + e % 4
-        const int edge = tile_edge(tb);
+        // register e holds key base + x, x = 8 (e / 4) + e % 4
         if (edge) {
-            const int base = tb + 32 * th + 4 * half;
+            const int base = list_tile(list, t) * kTile + 32 * sl + 4 * half;
             const int hi = p - base, past = p - a.window - base, first = a.sinks - base;
 #pragma unroll
             for (int e = 0; e < 16; e++) {
                 const int x = 8 * (e >> 2) + (e & 3);
-                if (!(x <= hi && (x > past || x < first))) s[e] = -INFINITY;
+                s[e] = (x <= hi) & ((x > past) | (x < first)) ? s[e] : -INFINITY;
             }
             if (edge == 2) {
                 const int32_t* ids = lds.pid + ((t - c0) << log2T);
 #pragma unroll
                 for (int e = 0; e < 16; e++)
-                    if (ids[(32 * th + 4 * half + 8 * (e >> 2) + (e & 3)) >> log2S] < 0) s[e] = -INFINITY;
+                    s[e] = ids[(32 * sl + 4 * half + 8 * (e >> 2) + (e & 3)) >> log2S] < 0 ? -INFINITY : s[e];
             }
         }
         // the row's maximum: lane-local, then across the lane halves; the running maximum moves only when a
@@ -446,7 +474,7 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
         const float ref = m_run == -INFINITY ? 0.0f : m_run;
         constexpr int NJ = 2 * DT, VPD = 4;
         auto vread = [&](int j) {
-            const int c = j / DT, t2 = j % DT;  // 16-token chunk of the wave's keys, d-tile
+            const int c = j / DT, t2 = j % DT;  // 16-token chunk of the keys, d-tile
             i16x4 vq[2];
 #pragma unroll
             for (int qh = 0; qh < 2; qh++)
@@ -481,8 +509,8 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
     };
 
     // Tile t: wait for its copies (and only those), barrier (tile visible; the buffer that the next copies
-    // fill no longer read), start those of tile t + PF, multiply.
-    const bool active = __builtin_amdgcn_readfirstlane(rg) * 32 < M;
+    // fill no longer read), start those of tile t + NBUF - 1, multiply. (The first NBUF start together.)
+    const bool active = rg * 32 < M;
     int buf = 0;
     for (int c0 = t0; c0 < t1; c0 += chunk_tiles) {
         const int c1 = min(t1, c0 + chunk_tiles);
@@ -490,72 +518,67 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
         stage(c0, c1);
         __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no other load pending when the ring starts
         __syncthreads();
+        holes = __builtin_amdgcn_readfirstlane(lds.holes) != 0;
 #pragma unroll
-        for (int x = 0; x < PF; x++)
-            if (c0 + x < c1) issue_tile(c0 + x, c0);
+        for (int x = 0; x < NBUF; x++)
+            if (c0 + x < c1) {
+                find_pages(c0 + x, c0);
+                issue_tile(c0 + x);
+            }
+        if (c0 + NBUF < c1) find_pages(c0 + NBUF, c0);
         for (int t = c0; t < c1; t++) {
-            const int newer = min(PF - 1, c1 - 1 - t);
-            if (newer >= 2) wait_vm<2 * IPW>();
-            else if (newer == 1) wait_vm<IPW>();
-            else wait_vm<0>();
-            clean_tile(t, c0, buf);
+            const int edge = tile_edge(list_tile(list, t) * kTile);
+            wait_tiles<NBUF - 1, IPW>(min(t == c0 ? NBUF - 1 : NBUF - 2, c1 - 1 - t));
+            if (edge != 0 && my_tensor == 1) clean_tile(t, c0, buf, edge);
             __syncthreads();
-            if (t + PF < c1) issue_tile(t + PF, c0);
-            if (active) compute_tile(t, c0, buf);
+            if (t > c0 && t + NBUF - 1 < c1) {
+                issue_tile(t + NBUF - 1);
+                if (t + NBUF < c1) find_pages(t + NBUF, c0);
+            }
+            if (active)
+                for (int sl = th; sl < 2; sl += parts) compute_half(t, c0, buf, sl, edge);
             buf = buf + 1 == NBUF ? 0 : buf + 1;
         }
         ibuf = buf;
     }
-    static_assert(PF <= 3, "the waits above");
 
+    // The parts of a row group hold the same (row, dim) elements in the same lanes and registers; each parks
+    // the d-tiles that the other one finishes in the ring.
     float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-    // merge the TS parts of a row group; wave th finishes d-tiles th, th + TS, ..
-    constexpr int DO = (DT + TS - 1) / TS;
-    f32x16 of[DO];
-    if constexpr (TS > 1) {
+    if (parts == 2) {
         __syncthreads();  // (the ring is free)
         f32x4* park = (f32x4*)lds.park + lane;
-        if (active) {
+        lds.ml[w][0][lane] = m_run;
+        lds.ml[w][1][lane] = l_tot;
+        auto put = [&](int from) {
 #pragma unroll
-            for (int t = 0; t < DT; t++)
+            for (int t = 0; t < DT / 2; t++)
 #pragma unroll
                 for (int g = 0; g < 4; g++)
-                    park[((w * DT + t) * 4 + g) * 64] = f32x4{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]};
-            lds.ml[w][0][lane] = m_run;
-            lds.ml[w][1][lane] = l_tot;
-        }
+                    park[((w * (DT / 2) + t) * 4 + g) * 64] = f32x4{o[from + t][4 * g], o[from + t][4 * g + 1],
+                                                                    o[from + t][4 * g + 2], o[from + t][4 * g + 3]};
+        };
+        if (th) put(0);
+        else put(DT / 2);
         __syncthreads();
-        if (active) {
-            float mm = -INFINITY, wt[TS];
-            l_tot = 0.0f;
+        const float m2 = lds.ml[w ^ 1][0][lane], l2 = lds.ml[w ^ 1][1][lane], mm = fmaxf(m_run, m2);
+        // (a part whose scores are all NaN has no maximum, but its sum counts)
+        const float a1 = m_run == -INFINITY ? (l_tot != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f((m_run - mm) * a.scale_log2);
+        const float a2 = m2 == -INFINITY ? (l2 != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f((m2 - mm) * a.scale_log2);
+        auto get = [&](int from) {
 #pragma unroll
-            for (int x = 0; x < TS; x++) mm = fmaxf(mm, lds.ml[rg * TS + x][0][lane]);
+            for (int t = 0; t < DT / 2; t++)
 #pragma unroll
-            for (int x = 0; x < TS; x++) {
-                const float mx = lds.ml[rg * TS + x][0][lane], lx = lds.ml[rg * TS + x][1][lane];
-                // (a part whose scores are all NaN has no maximum, but its sum counts)
-                wt[x] = mx == -INFINITY ? (lx != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f((mx - mm) * a.scale_log2);
-                l_tot += lx * wt[x];
-            }
-            m_run = mm;
+                for (int g = 0; g < 4; g++) {
+                    const f32x4 v = park[(((w ^ 1) * (DT / 2) + t) * 4 + g) * 64];
 #pragma unroll
-            for (int k = 0; k < DO; k++) {
-                of[k] = f32x16{};
-                const int t = th + k * TS;
-                if (t >= DT) continue;
-#pragma unroll
-                for (int x = 0; x < TS; x++)
-#pragma unroll
-                    for (int g = 0; g < 4; g++) {
-                        const f32x4 v = park[(((rg * TS + x) * DT + t) * 4 + g) * 64];
-#pragma unroll
-                        for (int e = 0; e < 4; e++) of[k][4 * g + e] += v[e] * wt[x];
-                    }
-            }
-        }
-    } else {
-#pragma unroll
-        for (int t = 0; t < DT; t++) of[t] = o[t];
+                    for (int e = 0; e < 4; e++) o[from + t][4 * g + e] = o[from + t][4 * g + e] * a1 + v[e] * a2;
+                }
+        };
+        if (th) get(DT / 2);
+        else get(0);
+        l_tot = l_tot * a1 + l2 * a2;
+        m_run = mm;
     }
     if (active && row_ok) {
         const float inv = l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
@@ -564,21 +587,20 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
         const bool whole = t1 - t0 == list.nt;
         const size_t prow = (size_t)sp * a.total_q * a.Hq + orow;
 #pragma unroll
-        for (int k = 0; k < DO; k++) {
-            const int t = th + k * TS;
-            if (t >= DT) continue;
+        for (int t = 0; t < DT; t++) {
+            if (parts == 2 && t / (DT / 2) != th) continue;
 #pragma unroll
             for (int g = 0; g < 4; g++) {
                 const int d0 = t * 32 + 8 * g + 4 * half;
                 if (whole) {
                     bf16x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; e++) v[e] = (__bf16)(of[k][4 * g + e] * inv);
+                    for (int e = 0; e < 4; e++) v[e] = (__bf16)(o[t][4 * g + e] * inv);
                     *(bf16x4*)((uint16_t*)a.out + orow * HD + d0) = v;
                 } else {
                     f32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; e++) v[e] = of[k][4 * g + e] * inv;
+                    for (int e = 0; e < 4; e++) v[e] = o[t][4 * g + e] * inv;
                     *(f32x4*)(a.part_o + prow * HD + d0) = v;
                 }
             }
@@ -590,16 +612,16 @@ __global__ __launch_bounds__(RG * TS * 64, 2) void window_bf16_kernel(WindowArgs
     }
     if (lds.dirty) {  // (written before a barrier that all have passed)
         __syncthreads();
-        redo_rows<HD>(a, i, h, sp, row0, M, q0, L, list, TT, t0, t1);
+        redo_rows<HD>(a, i, h, sp, row0, M, q0, L, list, t0, t1);
     }
 }
 
 // The splits of the divided lists: one thread per (row, 4 dims).
-__global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a, int TT) {
+__global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a) {
     const int SL = a.HD / 4, i = blockIdx.y;
     int q0, k_i, kv_len;
     if (!load_request(a, i, q0, k_i, kv_len)) return;
-    const KeyList list = key_list(a.window, a.sinks, TT, kv_len - k_i, k_i);
+    const KeyList list = key_list(a.window, a.sinks, kTile, kv_len - k_i, k_i);
     if (list.nt <= a.split_tiles) return;
     const int n = (list.nt + a.split_tiles - 1) / a.split_tiles;
     const long long u = (long long)blockIdx.x * 256 + threadIdx.x;
@@ -688,27 +710,25 @@ hipError_t launch_window(const sv_window_desc& w, const WindowPlan& plan, const 
         return hipGetLastError();
     }
     const dim3 grid(8 * a.per_xcd * plan.row_blocks);
-    const int tps = 512 / d.head_dim;  // tokens per 1 KB segment
-#define SV_WINDOW(HD, RG, TS, NB, LANE) \
-    hipLaunchKernelGGL((window_bf16_kernel<HD, RG, TS, NB, LANE>), grid, dim3(RG * TS * 64), 0, stream, a)
-#define SV_WINDOW_SHAPE(HD, LANE) \
-    if (plan.row_groups == 1) SV_WINDOW(HD, 1, 4, 2, LANE); \
-    else if (plan.row_groups == 2) SV_WINDOW(HD, 2, 2, 3, LANE); \
-    else SV_WINDOW(HD, 4, 1, 4, LANE)
-    if (d.head_dim == 128) {
-        if (d.page_size >= tps) { SV_WINDOW_SHAPE(128, false); }
-        else { SV_WINDOW_SHAPE(128, true); }
+#define SV_WINDOW(HD, NW, NB, PM) \
+    hipLaunchKernelGGL((window_bf16_kernel<HD, NW, NB, Pages::PM>), grid, dim3(NW * 64), 0, stream, a)
+#define SV_WINDOW_PAGES(HD, NW, NB) \
+    if (d.page_size >= kTile) SV_WINDOW(HD, NW, NB, kTile); \
+    else if (d.page_size >= 512 / HD) SV_WINDOW(HD, NW, NB, kSegment); \
+    else SV_WINDOW(HD, NW, NB, kLane)
+    if (plan.waves == 4) {
+        if (d.head_dim == 128) { SV_WINDOW_PAGES(128, 4, 2); }
+        else { SV_WINDOW_PAGES(64, 4, 4); }
     } else {
-        if (d.page_size >= tps) { SV_WINDOW_SHAPE(64, false); }
-        else { SV_WINDOW_SHAPE(64, true); }
+        if (d.head_dim == 128) { SV_WINDOW_PAGES(128, 8, 4); }
+        else { SV_WINDOW_PAGES(64, 8, 4); }
     }
-#undef SV_WINDOW_SHAPE
+#undef SV_WINDOW_PAGES
 #undef SV_WINDOW
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.splits == 1) return e;
     const long long slices = (long long)d.block * d.num_q_heads * (d.head_dim / 4);
-    hipLaunchKernelGGL(window_merge_kernel, dim3((unsigned)((slices + 255) / 256), d.num_reqs), dim3(256), 0, stream, a,
-                       plan.tile);
+    hipLaunchKernelGGL(window_merge_kernel, dim3((unsigned)((slices + 255) / 256), d.num_reqs), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

@@ -337,20 +337,18 @@ WindowPlan plan_window(const sv_window_desc& w) {
     p.splits = 1;
     p.split_tiles = 0x7FFFFFFF;
     if (d.dtype == SV_F32) return p;
-    // four waves: (32-row group, 32-key part of a tile)
-    p.row_groups = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-    p.tile = 32 * (4 / p.row_groups);
-    p.row_blocks = (int)((rows + 32 * p.row_groups - 1) / (32 * p.row_groups));
+    p.waves = rows <= 128 ? 4 : 8;
+    p.row_blocks = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
     // the longest list: the first tokens' tiles, and the window's with the other rows', which may start
     // inside a tile
+    constexpr long long T = 64;
     const long long span = std::min<long long>(d.max_kv_len, (long long)w.window + d.block - 1);
     const long long head = std::min<long long>(d.max_kv_len, w.sinks);
-    const long long tiles = std::min((d.max_kv_len + p.tile - 1LL) / p.tile,
-                                     (head + p.tile - 1) / p.tile + (span + p.tile - 2) / p.tile + 1);
+    const long long tiles = std::min((d.max_kv_len + T - 1) / T, (head + T - 1) / T + (span + T - 2) / T + 1);
     const long long units = (long long)d.num_reqs * d.num_kv_heads * p.row_blocks;
     long long per = tiles;
-    if (d.kv_split > 0) per = std::max<long long>(1, d.kv_split / p.tile);
-    else if (units < 512) per = std::max<long long>((256 + p.tile - 1) / p.tile, (tiles * units + 511) / 512);
+    if (d.kv_split > 0) per = std::max<long long>(1, d.kv_split / T);
+    else if (units < 512) per = std::max<long long>(4, (tiles * units + 511) / 512);
     p.split_tiles = (int)std::min(per, tiles);
     p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
     if (p.splits > 1) {

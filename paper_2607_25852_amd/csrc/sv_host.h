@@ -60,10 +60,9 @@ struct CompactPlan {
     size_t chunk_live, move_of, ws_bytes;
 };
 struct WindowPlan {
-    int row_groups;   // 32-row groups per workgroup (bf16): 1, 2 or 4
-    int tile;         // keys per tile
-    int row_blocks;   // row blocks of row_groups * 32 rows per (request, kv-head)
-    int splits, split_tiles;  // splits of every key list, tiles of each
+    int waves;        // waves per workgroup (bf16): 4 or 8, of 32 query rows each
+    int row_blocks;   // row blocks of waves * 32 rows per (request, kv-head)
+    int splits, split_tiles;  // splits of every key list, tiles of 64 keys of each
     size_t part_o_bytes, ws_bytes;
 };
 AttnPlan plan_attn(const sv_attn_desc& d);
