@@ -11,6 +11,7 @@
 #include "attn_tile.h"
 #include "rows.h"
 #include "sv_internal.h"
+#include "window_list.h"
 
 namespace sv {
 namespace {
@@ -33,20 +34,6 @@ struct WindowArgs {
     int nrb, per_xcd;         // row blocks per (request, kv-head); (request, split, kv-head) per XCD
     float scale, scale_log2;  // sm_scale, sm_scale * log2(e)
 };
-
-// The keys of a request with k rows after L committed tokens, in tiles of TT tokens
-struct KeyList {
-    int ns;  // tiles 0 .. ns-1 hold the first positions
-    int ft;  // then tiles from ft on
-    int nt;  // tiles in all
-};
-__device__ inline KeyList key_list(int window, int sinks, int TT, int L, int k) {
-    const int first = max(0, L - window + 1);
-    const int ns = (int)(((unsigned)min(sinks, first) + (unsigned)TT - 1) / (unsigned)TT);
-    const int ft = max(first / TT, ns);
-    return KeyList{ns, ft, ns + (L + k - 1) / TT - ft + 1};
-}
-__device__ inline int list_tile(const KeyList& x, int t) { return t < x.ns ? t : x.ft + (t - x.ns); }
 
 // the request's packing and key count; false: not sound
 __device__ inline bool load_request(const WindowArgs& a, int i, int& q0, int& k_i, int& kv_len) {
@@ -76,55 +63,54 @@ __device__ inline void store1(uint16_t* p, float f) { *p = f2bf(f); }
 // step, .. < t1 of its request's list. Leaves the softmax state (m, l) and o[e] for dim lane + 64 e.
 // Every key is used by itself: what a row does not see is not read.
 template <typename T>
-__device__ void wave_row(const WindowArgs& a, const T* qp, const int32_t* pt, int h, int p, const KeyList& list, int TT,
+__device__ void wave_row(const WindowArgs& a, const T* qp, const int32_t* pt, int h, int p, const KeyList& list,
                          int t, int t1, int step, float& m, float& l, float (&o)[4]) {
     const int lane = threadIdx.x & 63, HD = a.HD, P = 1 << a.log2P;
     m = -INFINITY, l = 0.0f;
 #pragma unroll
     for (int e = 0; e < 4; e++) o[e] = 0.0f;
-    for (; t < t1; t += step)
-        for (int at = 0; at < TT; at += 64) {
-            const int s = list_tile(list, t) * TT + at + lane;
-            float z = -INFINITY;
-            size_t off = 0;
-            bool ok = at + lane < TT && s <= p && (s < a.sinks || s > p - a.window);
+    for (; t < t1; t += step) {
+        const int s = list_tile(list, t) * kTile + lane;
+        float z = -INFINITY;
+        size_t off = 0;
+        bool ok = s <= p && (s < a.sinks || s > p - a.window);
+        if (ok) {
+            const int col = s >> a.log2P, pg = col < a.maxp ? pt[col] : -1;
+            ok = pg >= 0 && pg < a.num_pages;
             if (ok) {
-                const int col = s >> a.log2P, pg = col < a.maxp ? pt[col] : -1;
-                ok = pg >= 0 && pg < a.num_pages;
-                if (ok) {
-                    off = ((((size_t)pg * a.Hkv + h) << a.log2P) + (s & (P - 1))) * HD;
-                    float dot = 0.0f;
-                    for (int e = 0; e < HD; e += 4) {
-                        const f32x4 x = Vec4<T>::get((const T*)a.kc + off + e), y = Vec4<T>::get(qp + e);
-                        dot += x[0] * y[0] + x[1] * y[1] + x[2] * y[2] + x[3] * y[3];
-                    }
-                    z = dot * a.scale;
+                off = ((((size_t)pg * a.Hkv + h) << a.log2P) + (s & (P - 1))) * HD;
+                float dot = 0.0f;
+                for (int e = 0; e < HD; e += 4) {
+                    const f32x4 x = Vec4<T>::get((const T*)a.kc + off + e), y = Vec4<T>::get(qp + e);
+                    dot += x[0] * y[0] + x[1] * y[1] + x[2] * y[2] + x[3] * y[3];
                 }
-            }
-            float mx = z;
-            for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
-            const float m_new = fmaxf(m, mx);
-            if (m_new == -INFINITY && !__any(ok && z != z)) continue;
-            const float alpha = m == -INFINITY ? 0.0f : expf(m - m_new);
-            const float w = ok ? expf(z - m_new) : 0.0f;
-            float ws = w;
-            for (int x = 32; x > 0; x >>= 1) ws += __shfl_xor(ws, x, 64);
-            l = l * alpha + ws;
-            m = m_new;
-#pragma unroll
-            for (int e = 0; e < 4; e++) o[e] *= alpha;
-            uint64_t todo = __ballot(ok);
-            while (todo) {
-                const int j = __builtin_ctzll(todo);
-                todo &= todo - 1;
-                const float wj = __shfl(w, j, 64);
-                const size_t offj = ((size_t)(uint32_t)__shfl((int)(off >> 32), j, 64) << 32) |
-                                    (uint32_t)__shfl((int)(uint32_t)off, j, 64);
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (lane + 64 * e < HD) o[e] += wj * load1((const T*)a.vc + offj + lane + 64 * e);
+                z = dot * a.scale;
             }
         }
+        float mx = z;
+        for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
+        const float m_new = fmaxf(m, mx);
+        if (m_new == -INFINITY && !__any(ok && z != z)) continue;
+        const float alpha = m == -INFINITY ? 0.0f : expf(m - m_new);
+        const float w = ok ? expf(z - m_new) : 0.0f;
+        float ws = w;
+        for (int x = 32; x > 0; x >>= 1) ws += __shfl_xor(ws, x, 64);
+        l = l * alpha + ws;
+        m = m_new;
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] *= alpha;
+        uint64_t todo = __ballot(ok);
+        while (todo) {
+            const int j = __builtin_ctzll(todo);
+            todo &= todo - 1;
+            const float wj = __shfl(w, j, 64);
+            const size_t offj = ((size_t)(uint32_t)__shfl((int)(off >> 32), j, 64) << 32) |
+                                (uint32_t)__shfl((int)(uint32_t)off, j, 64);
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                if (lane + 64 * e < HD) o[e] += wj * load1((const T*)a.vc + offj + lane + 64 * e);
+        }
+    }
 }
 
 // fp32: one workgroup of four waves per (query row, head); wave w takes every fourth tile of 64 keys,
@@ -144,10 +130,10 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WindowArgs a) {
     int q0, k_i, kv_len;
     if (!load_request(a, lo, q0, k_i, kv_len) || row < q0 || row >= q0 + k_i) return;
     const int p = kv_len - k_i + (row - q0);
-    const KeyList list = key_list(a.window, a.sinks, 64, p, 1);
+    const KeyList list = key_list(a.window, a.sinks, p, 1);
     float o[4], m, l;
     wave_row<T>(a, (const T*)a.q + ((size_t)row * a.Hq + head) * HD, a.page_table + (size_t)lo * a.maxp, head / a.G, p,
-                list, 64, wv, list.nt, 4, m, l, o);
+                list, wv, list.nt, 4, m, l, o);
 #pragma unroll
     for (int e = 0; e < 4; e++) s_o[wv][e][lane] = o[e];
     if (lane == 0) {
@@ -178,7 +164,7 @@ __global__ __launch_bounds__(256) void window_rows_kernel(WindowArgs a) {
 // A workgroup of NW waves takes one (request, split, kv-head, row block): up to NW * 32 query rows of the
 // kv-head group (row r: position j = r / G, head r % G) against the split's tiles of 64 keys. Where the rows
 // fill half of the waves or less, two waves share 32 rows and take the halves of every tile
-// (parts = 2), else a wave takes both halves one after the other. As in attn.hip, S^T = K Q^T puts
+// (PARTS = 2), else a wave takes both halves. As in attn.hip, S^T = K Q^T puts
 // the scores of a query row into one lane pair, and P^T is then in the operand layout of
 // O^T = V^T P^T, with V read transposed from LDS. K and V tiles come through the page table into an LDS
 // ring by direct loads while earlier tiles are multiplied; the parts of a row are merged at the end.
@@ -200,30 +186,29 @@ struct WindowLds {
     float ml[NW][2][64];
     int32_t pid[kPageSlots];
     int32_t holes;  // a page that the list needs is missing
-    int32_t dirty;  // a value that only some rows see was not finite
 };
 
-// the rows of a row block one by one (rare: see `dirty`)
+// The outputs of rows r0 .. r1-1 of a row block once more, one by one, by one wave: dims d0 .. d1-1. A value that is
+// not finite reaches every row of its tile (0 * inf), those too that do not see it, so the rows of a
+// wave that finds such a result are done again from the definition. (Scores have no such neighbours.)
 template <int HD>
-__device__ __noinline__ void redo_rows(WindowArgs a, int i, int h, int sp, int row0, int M, int q0, int L,
-                                       KeyList list, int t0, int t1) {
-    const int lane = threadIdx.x & 63, waves = blockDim.x >> 6;
-    for (int r = threadIdx.x >> 6; r < M; r += waves) {
+__device__ __noinline__ void redo_rows(WindowArgs a, int i, int h, int sp, int row0, int r0, int r1, int q0, int L,
+                                       KeyList list, int t0, int t1, int d0, int d1) {
+    const int lane = threadIdx.x & 63;
+    for (int r = r0; r < r1; r++) {
         const int rr = row0 + r, jq = rr / a.G, head = h * a.G + rr % a.G;
         const size_t orow = (size_t)(q0 + jq) * a.Hq + head;
         float o[4], m, l;
-        wave_row<uint16_t>(a, (const uint16_t*)a.q + orow * HD, a.page_table + (size_t)i * a.maxp, h, L + jq, list, kTile,
-                           t0, t1, 1, m, l, o);
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l, lse = l == 0.0f ? -INFINITY : m + logf(l);
-        const bool whole = t1 - t0 == list.nt;
+        wave_row<uint16_t>(a, (const uint16_t*)a.q + orow * HD, a.page_table + (size_t)i * a.maxp, h, L + jq, list, t0, t1, 1,
+                           m, l, o);
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const bool whole = a.splits == 1 || t1 - t0 == list.nt;
         const size_t prow = (size_t)sp * a.total_q * a.Hq + orow;
         for (int e = 0; e < HD / 64; e++) {
-            if (whole) ((uint16_t*)a.out)[orow * HD + lane + 64 * e] = f2bf(o[e] * inv);
-            else a.part_o[prow * HD + lane + 64 * e] = o[e] * inv;
-        }
-        if (lane == 0) {
-            if (!whole) a.part_lse[prow] = lse * kLog2e;
-            else if (a.lse) a.lse[orow] = lse;
+            const int d = lane + 64 * e;
+            if (d < d0 || d >= d1) continue;
+            if (whole) ((uint16_t*)a.out)[orow * HD + d] = f2bf(o[e] * inv);
+            else a.part_o[prow * HD + d] = o[e] * inv;
         }
     }
 }
@@ -239,8 +224,11 @@ __device__ inline void wait_tiles(int newer) {
     }
 }
 
-template <int HD, int NW, int NBUF, Pages PM>
-__global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
+// One item, its waves divided into row groups of PARTS waves
+template <int HD, int NW, int NBUF, Pages PM, int PARTS>
+__device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, NW, NBUF>& lds, int i, int h, int sp,
+                                            int row0, int q0, int L, int M, int last, const KeyList& list, int t0,
+                                            int t1) {
     constexpr int CPR = HD / 8;             // 16-byte chunks per token row
     constexpr int TPS = 1024 / (HD * 2);    // tokens per 1 KB DMA segment
     constexpr int NSEG = kTile / TPS;       // segments per tensor per tile
@@ -249,29 +237,7 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
     constexpr int KK = HD / 16;             // MFMA k-steps over the head dim
     constexpr int DT = HD / 32;             // output d-tiles
     constexpr int log2T64 = 6;
-    static_assert(kTile == 1 << log2T64, "tile");
-    __shared__ __attribute__((aligned(16))) WindowLds<HD, NW, NBUF> lds;
-
-    // neighbouring workgroups go to the XCDs in turn: each takes a run of (request, split, kv-head)s, whose heads
-    // share pages, and the row blocks of one follow each other
-    // (the quotients of vector divisions, back in scalar registers: the copies' addresses need them there)
-    auto scalar = [](unsigned x) { return __builtin_amdgcn_readfirstlane((int)x); };
-    const unsigned slot = blockIdx.x / 8;
-    const int ux = scalar(slot / (unsigned)a.nrb), rb = scalar(slot % (unsigned)a.nrb);
-    const unsigned unit = (blockIdx.x % 8) * (unsigned)a.per_xcd + (unsigned)ux;
-    if (ux >= a.per_xcd || unit >= (unsigned)a.R * (unsigned)a.splits * (unsigned)a.Hkv) return;
-    const int h = scalar(unit % (unsigned)a.Hkv), is = scalar(unit / (unsigned)a.Hkv);
-    const int sp = scalar((unsigned)is % (unsigned)a.splits), i = scalar((unsigned)is / (unsigned)a.splits);
-    const int row0 = rb * NW * 32;
-    int q0, k_i, kv_len;
-    if (!load_request(a, i, q0, k_i, kv_len)) return;
-    const int M = min(a.G * k_i - row0, NW * 32);
-    if (M <= 0) return;
-    const int L = kv_len - k_i, last = kv_len - 1;  // the first and the last row's position
-    const KeyList list = key_list(a.window, a.sinks, kTile, L, k_i);
-    const int t0 = sp * a.split_tiles, t1 = min(list.nt, t0 + a.split_tiles);
-    if (t0 >= t1) return;
-
+    static_assert(kTile == 1 << log2T64 && kTile == kWindowTile, "tile");
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int32_t* __restrict__ pt = a.page_table + (size_t)i * a.maxp;
     const int log2S = min(a.log2P, log2T64), log2T = log2T64 - log2S;  // tokens per page slot, slots per tile
@@ -288,17 +254,16 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
         }
         if (hole) lds.holes = 1;
     };
-    if (tid == 0) lds.holes = lds.dirty = 0;
+    if (tid == 0) lds.holes = 0;
 
-    const int parts = M <= NW * 16 ? 2 : 1;
-    const int rg = parts == 2 ? w >> 1 : w, th = parts == 2 ? w & 1 : 0;
+    const int rg = w / PARTS, th = w % PARTS;
     const int r = rg * 32 + (lane & 31), half = lane >> 5;
     const bool row_ok = r < M;
     const int rr = row0 + (row_ok ? r : 0);  // row within the request's kv-head group
     const int jq = rr / a.G, head = h * a.G + rr % a.G;
     const int p = L + jq;  // the row's position
 
-    // per-lane element offsets of the V^T transpose reads (attn.hip)
+    // per-lane byte offsets of the V^T transpose reads (attn.hip)
     int vofs[2][DT];
     {
         const int g = lane >> 4, jl = lane & 15;
@@ -308,7 +273,7 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
 #pragma unroll
             for (int t = 0; t < DT; t++) {
                 const int dd = 32 * t + 16 * (g & 1) + 4 * (jl & 3);
-                vofs[qh][t] = tl * HD + (((dd >> 3) ^ (swz(tl) & (CPR - 1))) << 3) + (dd & 7);
+                vofs[qh][t] = (th * 32 * HD + tl * HD + (((dd >> 3) ^ (swz(tl) & (CPR - 1))) << 3) + (dd & 7)) * 2;
             }
         }
     }
@@ -331,14 +296,14 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
     // page reads page 0 (which exists); tokens that no row sees are masked out of the scores and
     // zeroed in V, whatever was read.
     const int seg0 = (w * IPW) % NSEG, my_tensor = (w * IPW) / NSEG;
-    uint32_t voff[IPW];  // bytes from the tile (kTile) or the segment
-    int tk[IPW];
+    // (the swizzle repeats every 16 tokens)
+    constexpr int NV = 16 / TPS < IPW ? 16 / TPS : IPW;
+    uint32_t voff[NV];  // bytes from the tile's first segment of this wave (kTile) or the segment
 #pragma unroll
-    for (int k = 0; k < IPW; k++) {
-        tk[k] = (seg0 + k) * TPS + lane / CPR;
-        voff[k] = (uint32_t)((PM == Pages::kTile ? tk[k] : lane / CPR) * HD +
-                             (((lane % CPR) ^ (swz(tk[k]) & (CPR - 1))) << 3)) * 2u;
-    }
+    for (int k = 0; k < NV; k++)
+        voff[k] = (uint32_t)(((PM == Pages::kTile ? k * TPS : 0) + lane / CPR) * HD +
+                             (((lane % CPR) ^ (swz((seg0 + k) * TPS + lane / CPR) & (CPR - 1))) << 3)) * 2u;
+    auto token = [&](int k) { return (seg0 + k) * TPS + lane / CPR; };  // of segment k, in the tile
     const char* cbase = (const char*)(my_tensor ? a.vc : a.kc);
     const uint32_t my_ring = (uint32_t)(uintptr_t)(my_tensor ? &lds.v[0][0] : &lds.k[0][0]) + (uint32_t)(seg0 * 1024);
     const int pmask = (1 << a.log2P) - 1;
@@ -353,112 +318,138 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
         const int32_t* ids = lds.pid + ((t - c0) << log2T);
         if constexpr (PM == Pages::kLane) {
 #pragma unroll
-            for (int k = 0; k < IPW; k++) pgv[k] = ids[tk[k] >> log2S];
+            for (int k = 0; k < IPW; k++) pgv[k] = ids[token(k) >> log2S];
         } else if constexpr (PM == Pages::kSegment) {
             pgv[0] = ids[((seg0 + (lane & (IPW - 1))) * TPS) >> log2S];
         } else {
             pgv[0] = ids[0];
         }
     };
-    auto issue_tile = [&](int t) {
-        const int tb = list_tile(list, t) * kTile;
-        const uint32_t lbuf = my_ring + (uint32_t)(ibuf * kTile * HD * 2);
-        ibuf = ibuf + 1 == NBUF ? 0 : ibuf + 1;
-        if constexpr (PM == Pages::kTile) {
-            const unsigned pg = max(__builtin_amdgcn_readfirstlane(pgv[0]), 0);
-            const char* base = cbase + pg * page_bytes + head_bytes + (uint32_t)(tb & pmask) * (HD * 2);
-#pragma unroll
-            for (int k = 0; k < IPW; k++) dma16s(voff[k], base, lbuf + 1024 * k);
-        } else {
-#pragma unroll
-            for (int k = 0; k < IPW; k++) {
-                if constexpr (PM == Pages::kLane) {
-                    const char* src = cbase;
-                    if (pgv[k] >= 0)
-                        src += (unsigned)pgv[k] * page_bytes + head_bytes + (uint32_t)((tb + tk[k]) & pmask) * (HD * 2) +
-                               (voff[k] - (uint32_t)(lane / CPR) * (HD * 2));
-                    dma16(src, lbuf + 1024 * k);
-                } else {
-                    const unsigned pg = max(__builtin_amdgcn_readlane(pgv[0], k), 0);
-                    dma16s(voff[k], cbase + pg * page_bytes + head_bytes +
-                                        (uint32_t)((tb + (seg0 + k) * TPS) & pmask) * (HD * 2), lbuf + 1024 * k);
-                }
-            }
-        }
-    };
-
     // what a tile at token tb needs: 0 nothing (every row sees all of it), 1 the mask, 2 mask and page look-up
     bool holes = false;
     auto tile_edge = [&](int tb) {
         return holes ? 2 : (tb + kTile - 1 <= L) & ((tb + kTile <= a.sinks) | (tb > last - a.window)) ? 0 : 1;
     };
-    // before the barrier that publishes an edge tile: the lanes that copied V rows which no row sees zero them (P
-    // is 0 there, but 0 * NaN is not), and rows that only some see are zeroed if they are not finite: the
-    // row block is then done again row by row
+    // Segments that no row sees are not fetched from memory: the first one of the cache is read again in
+    // their place (which keeps the count of loads per tile).
+    auto dead = [&](int s0, int s1) { return (s0 > last) | ((s0 >= a.sinks) & (s1 <= L - a.window)); };
+    auto issue_tile = [&](int t) {
+        const int tb = list_tile(list, t) * kTile;
+        const bool edge = tile_edge(tb) != 0;
+        const uint32_t lbuf = my_ring + (uint32_t)(ibuf * kTile * HD * 2);
+        ibuf = ibuf + 1 == NBUF ? 0 : ibuf + 1;
+        if constexpr (PM == Pages::kTile) {
+            const unsigned pg = max(__builtin_amdgcn_readfirstlane(pgv[0]), 0);
+            const char* base = cbase + pg * page_bytes + head_bytes + (uint32_t)((tb & pmask) + seg0 * TPS) * (HD * 2);
+            if (edge) {
+#pragma unroll
+                for (int k = 0; k < IPW; k++) {
+                    const int s0 = tb + (seg0 + k) * TPS;
+                    dma16s(voff[k % NV], dead(s0, s0 + TPS - 1) ? cbase : base + k / NV * (NV * TPS * HD * 2),
+                           lbuf + 1024 * k);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < IPW; k++) dma16s(voff[k % NV], base + k / NV * (NV * TPS * HD * 2), lbuf + 1024 * k);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < IPW; k++) {
+                const int s0 = tb + (seg0 + k) * TPS;
+                const bool skip = edge && dead(s0, s0 + TPS - 1);
+                if constexpr (PM == Pages::kLane) {
+                    const char* src = cbase;
+                    if (pgv[k] >= 0 && !skip)
+                        src += (unsigned)pgv[k] * page_bytes + head_bytes + (uint32_t)((tb + token(k)) & pmask) * (HD * 2) +
+                               (voff[k % NV] - (uint32_t)(lane / CPR) * (HD * 2));
+                    dma16(src, lbuf + 1024 * k);
+                } else {
+                    const unsigned pg = max(__builtin_amdgcn_readlane(pgv[0], k), 0);
+                    const char* base = cbase + pg * page_bytes + head_bytes + (uint32_t)(s0 & pmask) * (HD * 2);
+                    dma16s(voff[k % NV], skip ? cbase : base, lbuf + 1024 * k);
+                }
+            }
+        }
+    };
+
+    // before the barrier that publishes an edge tile, the lanes that copied V rows which no row sees zero them: P is
+    // 0 there, but 0 * NaN is not
     auto clean_tile = [&](int t, int c0, int buf, int edge) {
         const int tb = list_tile(list, t) * kTile;
 #pragma unroll
         for (int k = 0; k < IPW; k++) {
-            const int s = tb + tk[k];
-            u16x8* at = (u16x8*)((char*)lds.v[buf] + (seg0 + k) * 1024 + 16 * lane);
+            const int s0 = tb + (seg0 + k) * TPS, s1 = s0 + TPS - 1;  // the segment's keys
+            if (edge == 1 && (s1 <= last) & ((s1 < a.sinks) | (s0 > L - a.window))) continue;
+            const int s = tb + token(k);
             bool zero = (s > last) | ((s >= a.sinks) & (s <= L - a.window));
-            if (edge == 2) zero |= lds.pid[((t - c0) << log2T) + (tk[k] >> log2S)] < 0;
-            if (!zero && ((s > L) | ((s >= a.sinks) & (s <= last - a.window)))) {
-                const u16x8 v = *at;
-#pragma unroll
-                for (int e = 0; e < 8; e++) zero |= (v[e] & 0x7F80) == 0x7F80;
-                if (zero) lds.dirty = 1;
-            }
-            if (zero) *at = u16x8{};
+            if (edge == 2) zero |= lds.pid[((t - c0) << log2T) + (token(k) >> log2S)] < 0;
+            if (zero) *(u16x8*)((char*)lds.v[buf] + (seg0 + k) * 1024 + 16 * lane) = u16x8{};
         }
     };
 
-    const int sw = swz(lane & 31) & (CPR - 1);
-    // 32 keys of a tile, from key 32 sl on
-    auto compute_half = [&](int t, int c0, int buf, int sl, int edge) {
-        const uint16_t* vt = lds.v[buf] + sl * 32 * HD;
-        // S^T = K Q^T in two chains, operands read KPD products ahead
-        f32x16 s;
+    // LDS byte offsets of the operands inside a tile: K of k-step j of this lane's key, V^T (attn.hip)
+    uint32_t kofs[KK];
+#pragma unroll
+    for (int j = 0; j < KK; j++)
+        kofs[j] = (uint32_t)((th * 32 + (lane & 31)) * HD + (((2 * j + half) ^ (swz(lane & 31) & (CPR - 1))) << 3)) * 2u;
+    // One online-softmax step: this wave's NSB halves (32 keys each) of a tile. The products' operands are read
+    // from LDS a few products ahead; the scheduling barriers keep that order. With two halves, the
+    // exponents of the second are computed between the first half's products with V.
+    constexpr int NSB = 2 / PARTS;
+    auto compute_tile = [&](int t, int c0, int buf, int edge) {
+        const char* kt = (const char*)lds.k[buf];
+        const char* vt = (const char*)lds.v[buf];
+        constexpr int HB = 32 * HD * 2;  // bytes of half a tile
+        // S^T = K Q^T: the two halves are two chains
+        f32x16 s[NSB];
         {
-            const uint16_t* krow = lds.k[buf] + (sl * 32 + (lane & 31)) * HD;
-            constexpr int KPD = 4;
-            auto kread = [&](int j) { return __builtin_bit_cast(bf16x8, *(const u16x8*)(krow + (((2 * j + half) ^ sw) << 3))); };
+            constexpr int NF = NSB * KK, KPD = 4;
+            auto kread = [&](int j) {
+                return __builtin_bit_cast(bf16x8, *(const u16x8*)(kt + kofs[j / NSB] + (j % NSB) * HB));
+            };
             bf16x8 kb[KPD + 1];
-            f32x16 c0a = f32x16{}, c1a = f32x16{};
+#pragma unroll
+            for (int x = 0; x < NSB; x++) s[x] = f32x16{};
 #pragma unroll
             for (int j = 0; j < KPD; j++) kb[j] = kread(j);
 #pragma unroll
-            for (int j = 0; j < KK; j++) {
-                if (j + KPD < KK) kb[(j + KPD) % (KPD + 1)] = kread(j + KPD);
+            for (int j = 0; j < NF; j++) {
+                if (j + KPD < NF) kb[(j + KPD) % (KPD + 1)] = kread(j + KPD);
                 __builtin_amdgcn_sched_barrier(0);
-                if (j & 1) c1a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[j % (KPD + 1)], qf[j], c1a, 0, 0, 0);
-                else c0a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[j % (KPD + 1)], qf[j], c0a, 0, 0, 0);
+                s[j % NSB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[j % (KPD + 1)], qf[j / NSB], s[j % NSB], 0, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
-            s = c0a + c1a;
         }
-        // register e holds key base + x, x = 8 (e / 4) + e % 4
+        // register e of half x holds key base + 32 x + y, y = 8 (e / 4) + e % 4
         if (edge) {
-            const int base = list_tile(list, t) * kTile + 32 * sl + 4 * half;
+            const int base = list_tile(list, t) * kTile + 32 * th + 4 * half;
             const int hi = p - base, past = p - a.window - base, first = a.sinks - base;
 #pragma unroll
-            for (int e = 0; e < 16; e++) {
-                const int x = 8 * (e >> 2) + (e & 3);
-                s[e] = (x <= hi) & ((x > past) | (x < first)) ? s[e] : -INFINITY;
-            }
+            for (int x = 0; x < NSB; x++)
+#pragma unroll
+                for (int e = 0; e < 16; e++) {
+                    const int y = 32 * x + 8 * (e >> 2) + (e & 3);
+                    s[x][e] = (y <= hi) & ((y > past) | (y < first)) ? s[x][e] : -INFINITY;
+                }
             if (edge == 2) {
                 const int32_t* ids = lds.pid + ((t - c0) << log2T);
 #pragma unroll
-                for (int e = 0; e < 16; e++)
-                    s[e] = ids[(32 * sl + 4 * half + 8 * (e >> 2) + (e & 3)) >> log2S] < 0 ? -INFINITY : s[e];
+                for (int x = 0; x < NSB; x++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++)
+                        s[x][e] = ids[(32 * (th + x) + 4 * half + 8 * (e >> 2) + (e & 3)) >> log2S] < 0 ? -INFINITY : s[x][e];
             }
         }
         // the row's maximum: lane-local, then across the lane halves; the running maximum moves only when a
         // score passes it by more than 8 in log2 units, so the weights stay below 2^8
-        float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
+        float mx = fmaxf(fmaxf(s[0][0], s[0][1]), s[0][2]);
 #pragma unroll
-        for (int e = 3; e < 15; e += 2) mx = fmaxf(fmaxf(mx, s[e]), s[e + 1]);
-        mx = fmaxf(mx, s[15]);
+        for (int e = 3; e < 15; e += 2) mx = fmaxf(fmaxf(mx, s[0][e]), s[0][e + 1]);
+        mx = fmaxf(mx, s[0][15]);
+        if constexpr (NSB == 2) {
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) mx = fmaxf(fmaxf(mx, s[1][e]), s[1][e + 1]);
+        }
         {
             const auto sw2 = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
             mx = fmaxf(__uint_as_float(sw2[0]), __uint_as_float(sw2[1]));
@@ -472,40 +463,55 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
             m_run = m_new;
         }
         const float ref = m_run == -INFINITY ? 0.0f : m_run;
-        constexpr int NJ = 2 * DT, VPD = 4;
+        // O^T += V^T P^T: product j of half j / NJ, 16-key chunk (j % NJ) / DT, d-tile j % DT
+        constexpr int NJ = 2 * DT, NT = NSB * NJ, VPD = 4;
         auto vread = [&](int j) {
-            const int c = j / DT, t2 = j % DT;  // 16-token chunk of the keys, d-tile
             i16x4 vq[2];
 #pragma unroll
             for (int qh = 0; qh < 2; qh++)
-                vq[qh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(vt + 16 * c * HD + vofs[qh][t2]));
+                vq[qh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_i16x4*)(vt + vofs[qh][j % DT] + (j / NJ) * HB + ((j % NJ) / DT) * (16 * HD * 2)));
             return __builtin_shufflevector(vq[0], vq[1], 0, 1, 2, 3, 4, 5, 6, 7);
         };
         i16x8 vb[VPD + 1];
 #pragma unroll
         for (int j = 0; j < VPD; j++) vb[j] = vread(j);
         __builtin_amdgcn_sched_barrier(0);
-        float psum = 0.0f;
+        float psum[NSB];
+        bf16x8 pb[NSB][2];
+        auto weight = [&](int x, int e) {
+            s[x][e] = __builtin_amdgcn_exp2f((s[x][e] - ref) * a.scale_log2);
+            psum[x] += s[x][e];
+        };
+        auto pack = [&](int x) {
 #pragma unroll
-        for (int e = 0; e < 16; e++) {
-            s[e] = __builtin_amdgcn_exp2f((s[e] - ref) * a.scale_log2);
-            psum += s[e];
-        }
-        l_run += psum;
-        bf16x8 pb[2];
+            for (int cc = 0; cc < 2; cc++)
 #pragma unroll
-        for (int cc = 0; cc < 2; cc++)
+                for (int e = 0; e < 8; e++) pb[x][cc][e] = (__bf16)s[x][8 * cc + e];
+        };
 #pragma unroll
-            for (int e = 0; e < 8; e++) pb[cc][e] = (__bf16)s[8 * cc + e];
+        for (int x = 0; x < NSB; x++) psum[x] = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; e++) weight(0, e);
+        pack(0);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < NJ; j++) {
-            if (j + VPD < NJ) vb[(j + VPD) % (VPD + 1)] = vread(j + VPD);
+        for (int j = 0; j < NT; j++) {
+            if (j + VPD < NT) vb[(j + VPD) % (VPD + 1)] = vread(j + VPD);
             __builtin_amdgcn_sched_barrier(0);
-            o[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vb[j % (VPD + 1)]), pb[j / DT],
-                                                                o[j % DT], 0, 0, 0);
+            o[j % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vb[j % (VPD + 1)]),
+                                                                pb[j / NJ][(j % NJ) / DT], o[j % DT], 0, 0, 0);
+            if constexpr (NSB == 2) {
+                if (j < NJ) {
+#pragma unroll
+                    for (int x = 0; x < 16 / NJ; x++) weight(1, j * (16 / NJ) + x);
+                    if (j == NJ - 1) pack(1);
+                }
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
+#pragma unroll
+        for (int x = 0; x < NSB; x++) l_run += psum[x];
     };
 
     // Tile t: wait for its copies (and only those), barrier (tile visible; the buffer that the next copies
@@ -514,7 +520,7 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
     int buf = 0;
     for (int c0 = t0; c0 < t1; c0 += chunk_tiles) {
         const int c1 = min(t1, c0 + chunk_tiles);
-        __syncthreads();  // (holes, dirty cleared; page ids of the chunk before read)
+        __syncthreads();  // (holes cleared; page ids of the chunk before read)
         stage(c0, c1);
         __builtin_amdgcn_s_waitcnt(0x0F70);  // vmcnt(0): no other load pending when the ring starts
         __syncthreads();
@@ -535,8 +541,7 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
                 issue_tile(t + NBUF - 1);
                 if (t + NBUF < c1) find_pages(t + NBUF, c0);
             }
-            if (active)
-                for (int sl = th; sl < 2; sl += parts) compute_half(t, c0, buf, sl, edge);
+            if (active) compute_tile(t, c0, buf, edge);
             buf = buf + 1 == NBUF ? 0 : buf + 1;
         }
         ibuf = buf;
@@ -545,7 +550,7 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
     // The parts of a row group hold the same (row, dim) elements in the same lanes and registers; each parks
     // the d-tiles that the other one finishes in the ring.
     float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-    if (parts == 2) {
+    if constexpr (PARTS == 2) {
         __syncthreads();  // (the ring is free)
         f32x4* park = (f32x4*)lds.park + lane;
         lds.ml[w][0][lane] = m_run;
@@ -584,11 +589,11 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
         const float inv = l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
         const float lse2 = l_tot == 0.0f ? -INFINITY : m_run * a.scale_log2 + __log2f(l_tot);
         const size_t orow = (size_t)(q0 + jq) * a.Hq + head;
-        const bool whole = t1 - t0 == list.nt;
+        const bool whole = a.splits == 1 || t1 - t0 == list.nt;
         const size_t prow = (size_t)sp * a.total_q * a.Hq + orow;
 #pragma unroll
         for (int t = 0; t < DT; t++) {
-            if (parts == 2 && t / (DT / 2) != th) continue;
+            if (PARTS == 2 && t / (DT / 2) != th) continue;
 #pragma unroll
             for (int g = 0; g < 4; g++) {
                 const int d0 = t * 32 + 8 * g + 4 * half;
@@ -610,10 +615,44 @@ __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
             else if (a.lse) a.lse[orow] = lse2 * kLn2;
         }
     }
-    if (lds.dirty) {  // (written before a barrier that all have passed)
-        __syncthreads();
-        redo_rows<HD>(a, i, h, sp, row0, M, q0, L, list, t0, t1);
+    float odd = 0.0f;  // NaN where a result is not finite
+    if (active && row_ok) {
+#pragma unroll
+        for (int t = 0; t < DT; t++) {
+            if (PARTS == 2 && t / (DT / 2) != th) continue;
+#pragma unroll
+            for (int e = 0; e < 16; e++) odd = __builtin_fmaf(o[t][e], 0.0f, odd);
+        }
     }
+    if (__any(odd != odd))
+        redo_rows<HD>(a, i, h, sp, row0, rg * 32, min(M, rg * 32 + 32), q0, L, list, t0, t1, th * (HD / PARTS),
+                      (th + 1) * (HD / PARTS));
+}
+
+template <int HD, int NW, int NBUF, Pages PM>
+__global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
+    __shared__ __attribute__((aligned(16))) WindowLds<HD, NW, NBUF> lds;
+    // neighbouring workgroups go to the XCDs in turn: each takes a run of (request, split, kv-head)s, whose heads
+    // share pages, and the row blocks of one follow each other
+    // (the quotients of vector divisions, back in scalar registers: the copies' addresses need them there)
+    auto scalar = [](unsigned x) { return __builtin_amdgcn_readfirstlane((int)x); };
+    const unsigned slot = blockIdx.x / 8;
+    const int ux = scalar(slot / (unsigned)a.nrb), rb = scalar(slot % (unsigned)a.nrb);
+    const unsigned unit = (blockIdx.x % 8) * (unsigned)a.per_xcd + (unsigned)ux;
+    if (ux >= a.per_xcd || unit >= (unsigned)a.R * (unsigned)a.splits * (unsigned)a.Hkv) return;
+    const int h = scalar(unit % (unsigned)a.Hkv), is = scalar(unit / (unsigned)a.Hkv);
+    const int sp = scalar((unsigned)is % (unsigned)a.splits), i = scalar((unsigned)is / (unsigned)a.splits);
+    const int row0 = rb * NW * 32;
+    int q0, k_i, kv_len;
+    if (!load_request(a, i, q0, k_i, kv_len)) return;
+    const int M = min(a.G * k_i - row0, NW * 32);
+    if (M <= 0) return;
+    const int L = kv_len - k_i, last = kv_len - 1;  // the first and the last row's position
+    const KeyList list = key_list(a.window, a.sinks, L, k_i);
+    const int t0 = sp * a.split_tiles, t1 = min(list.nt, t0 + a.split_tiles);
+    if (t0 >= t1) return;
+    if (M <= NW * 16) window_item<HD, NW, NBUF, PM, 2>(a, lds, i, h, sp, row0, q0, L, M, last, list, t0, t1);
+    else window_item<HD, NW, NBUF, PM, 1>(a, lds, i, h, sp, row0, q0, L, M, last, list, t0, t1);
 }
 
 // The splits of the divided lists: one thread per (row, 4 dims).
@@ -621,7 +660,7 @@ __global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a) {
     const int SL = a.HD / 4, i = blockIdx.y;
     int q0, k_i, kv_len;
     if (!load_request(a, i, q0, k_i, kv_len)) return;
-    const KeyList list = key_list(a.window, a.sinks, kTile, kv_len - k_i, k_i);
+    const KeyList list = key_list(a.window, a.sinks, kv_len - k_i, k_i);
     if (list.nt <= a.split_tiles) return;
     const int n = (list.nt + a.split_tiles - 1) / a.split_tiles;
     const long long u = (long long)blockIdx.x * 256 + threadIdx.x;

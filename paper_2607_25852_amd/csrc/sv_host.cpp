@@ -9,6 +9,8 @@
 #include <cstdarg>
 #include <cstdio>
 
+#include "window_list.h"
+
 namespace sv {
 
 namespace {
@@ -339,12 +341,8 @@ WindowPlan plan_window(const sv_window_desc& w) {
     if (d.dtype == SV_F32) return p;
     p.waves = rows <= 128 ? 4 : 8;
     p.row_blocks = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
-    // the longest list: the first tokens' tiles, and the window's with the other rows', which may start
-    // inside a tile
-    constexpr long long T = 64;
-    const long long span = std::min<long long>(d.max_kv_len, (long long)w.window + d.block - 1);
-    const long long head = std::min<long long>(d.max_kv_len, w.sinks);
-    const long long tiles = std::min((d.max_kv_len + T - 1) / T, (head + T - 1) / T + (span + T - 2) / T + 1);
+    constexpr int T = kWindowTile;
+    const long long tiles = longest_list(w.window, w.sinks, d.block, d.max_kv_len);
     const long long units = (long long)d.num_reqs * d.num_kv_heads * p.row_blocks;
     long long per = tiles;
     if (d.kv_split > 0) per = std::max<long long>(1, d.kv_split / T);
