@@ -46,12 +46,19 @@ __device__ inline bool load_request(const WindowArgs& a, int i, int& q0, int& k_
 template <typename T> struct Vec4;
 template <> struct Vec4<float> {
     static __device__ f32x4 get(const float* p) { return *(const f32x4*)p; }
+    static __device__ void put(float* p, f32x4 x) { *(f32x4*)p = x; }
 };
 template <> struct Vec4<uint16_t> {
     static __device__ f32x4 get(const uint16_t* p) {
         const uint2 w = *(const uint2*)p;
         return f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
                      __uint_as_float(w.y & 0xFFFF0000u)};
+    }
+    static __device__ void put(uint16_t* p, f32x4 x) {
+        bf16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = (__bf16)x[e];
+        *(bf16x4*)p = v;
     }
 };
 __device__ inline float load1(const float* p) { return *p; }
@@ -113,49 +120,216 @@ __device__ void wave_row(const WindowArgs& a, const T* qp, const int32_t* pt, in
     }
 }
 
-// fp32: one workgroup of four waves per (query row, head); wave w takes every fourth tile of 64 keys,
-// and the waves' softmax states are merged at the end.
+// The outputs of rows r0 .. r1-1 of a row block once more, one by one, by one wave: dims d0 .. d1-1. A value that is
+// not finite reaches every row of its tile (0 * inf), those too that do not see it, so the rows of a
+// wave that finds such a result are done again from the definition. (Scores have no such neighbours.)
 template <typename T>
-__global__ __launch_bounds__(256) void window_rows_kernel(WindowArgs a) {
-    __shared__ float s_o[4][4][64];
-    __shared__ float s_ml[4][2];
-    const int wv = threadIdx.x >> 6, lane = threadIdx.x & 63, HD = a.HD;
-    const int row = blockIdx.x / a.Hq, head = blockIdx.x % a.Hq;
-    if (row >= a.qo[a.R]) return;
-    int lo = 0, hi = a.R - 1;  // the last request whose rows start at or before this one
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (a.qo[mid] <= row) lo = mid; else hi = mid - 1;
+__device__ __noinline__ void redo_rows(WindowArgs a, int i, int h, int sp, int row0, int r0, int r1, int q0, int L,
+                                       KeyList list, int t0, int t1, int d0, int d1) {
+    const int lane = threadIdx.x & 63, HD = a.HD;
+    for (int r = r0; r < r1; r++) {
+        const int rr = row0 + r, jq = rr / a.G, head = h * a.G + rr % a.G;
+        const size_t orow = (size_t)(q0 + jq) * a.Hq + head;
+        float o[4], m, l;
+        wave_row<T>(a, (const T*)a.q + orow * HD, a.page_table + (size_t)i * a.maxp, h, L + jq, list, t0, t1, 1, m, l, o);
+        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+        const bool whole = a.splits == 1 || t1 - t0 == list.nt;
+        const size_t prow = (size_t)sp * a.total_q * a.Hq + orow;
+        for (int e = 0; e < 4; e++) {
+            const int d = lane + 64 * e;
+            if (d < d0 || d >= d1) continue;
+            if (whole) store1((T*)a.out + orow * HD + d, o[e] * inv);
+            else a.part_o[prow * HD + d] = o[e] * inv;
+        }
     }
-    int q0, k_i, kv_len;
-    if (!load_request(a, lo, q0, k_i, kv_len) || row < q0 || row >= q0 + k_i) return;
-    const int p = kv_len - k_i + (row - q0);
-    const KeyList list = key_list(a.window, a.sinks, p, 1);
-    float o[4], m, l;
-    wave_row<T>(a, (const T*)a.q + ((size_t)row * a.Hq + head) * HD, a.page_table + (size_t)lo * a.maxp, head / a.G, p,
-                list, wv, list.nt, 4, m, l, o);
+}
+
+// What a workgroup works on: neighbouring workgroups go to the XCDs in turn, and each XCD takes a run of
+// (request, split, kv-head)s, whose heads share pages; the row blocks of one follow each other.
+struct Item {
+    int i, h, sp, row0, M;  // request, kv-head, split, first row of the kv-head group, rows
+    int q0, L, last;        // the request's first row; positions of its first and last row
+    int t0, t1;
+    KeyList list;
+};
+__device__ __forceinline__ bool find_item(const WindowArgs& a, int block_rows, Item& x) {
+    // (the quotients of vector divisions, back in scalar registers: the copies' addresses need them there)
+    auto scalar = [](unsigned v) { return __builtin_amdgcn_readfirstlane((int)v); };
+    const unsigned slot = blockIdx.x / 8;
+    const int ux = scalar(slot / (unsigned)a.nrb), rb = scalar(slot % (unsigned)a.nrb);
+    const unsigned unit = (blockIdx.x % 8) * (unsigned)a.per_xcd + (unsigned)ux;
+    if (ux >= a.per_xcd || unit >= (unsigned)a.R * (unsigned)a.splits * (unsigned)a.Hkv) return false;
+    x.h = scalar(unit % (unsigned)a.Hkv);
+    const int is = scalar(unit / (unsigned)a.Hkv);
+    x.sp = scalar((unsigned)is % (unsigned)a.splits);
+    x.i = scalar((unsigned)is / (unsigned)a.splits);
+    x.row0 = rb * block_rows;
+    int k_i, kv_len;
+    if (!load_request(a, x.i, x.q0, k_i, kv_len)) return false;
+    x.M = min(a.G * k_i - x.row0, block_rows);
+    if (x.M <= 0) return false;
+    x.L = kv_len - k_i;
+    x.last = kv_len - 1;
+    x.list = key_list(a.window, a.sinks, x.L, k_i);
+    x.t0 = x.sp * a.split_tiles;
+    x.t1 = min(x.list.nt, x.t0 + a.split_tiles);
+    return x.t0 < x.t1;
+}
+
+// ---------------------------------------------------------------------------------
+// fp32 MFMA kernel
+// ---------------------------------------------------------------------------------
+// A workgroup of four waves takes one item of up to 16 query rows; wave w has keys 16 w .. + 15 of every tile.
+// v_mfma_f32_16x16x4_f32 multiplies and adds in fp32. Its k index is free as long as both operands agree, which
+// lets every lane load 16 bytes at a time straight into the operands (lane = 16 q + n):
+//   scores S^T = K Q^T: step (b, c) takes dim 16 b + 4 q + c of key n and of row n;
+//   lane 16 q + n gets the scores of row n with keys 4 q + e, e = 0..3;
+//   O^T = V^T P^T: step e takes key 4 q + e, so P^T is where the scores were left; tile (g, c) of the
+//   output has dims 64 g + 4 n + c, and lane 16 q + n gets dims 64 g + 16 q + 4 e + c of row n.
+// Keys that no row sees are not loaded. Bound by the latency of a tile's loads (page, K and V) and by the chain of
+// its products (fp32 products run at a sixteenth of the bf16 rate). With 32 rows per wave (twice the
+// products per load, half the waves) 8 requests of 5 positions and windows of 512 took 26.8 us, with 16
+// rows 20.3 us.
+template <int DG>
+__global__ __launch_bounds__(256, DG == 4 ? 1 : 2) void window_f32_kernel(WindowArgs a) {
+    constexpr int NW = 4, NB = 4 * DG;  // waves; 16-dim blocks of the scores' sum
+    __shared__ float s_o[NW][DG * 4][4][64];
+    __shared__ float s_ml[NW][2][64];
+    Item x;
+    if (!find_item(a, 16, x)) return;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int n = lane & 15, q = lane >> 4, HD = a.HD;
+    const int32_t* __restrict__ pt = a.page_table + (size_t)x.i * a.maxp;
+    // the page of this lane's key (n) of tile t; -1: no row sees it, or it does not exist
+    auto page_of = [&](int t) {
+        const int s = list_tile(x.list, t) * kTile + 16 * w + n, col = s >> a.log2P;
+        const bool seen = (s <= x.last) & ((s < a.sinks) | (s > x.L - a.window)) & (col < a.maxp);
+        const int pg = seen ? pt[col] : -1;
+        return pg < a.num_pages ? pg : -1;
+    };
+    int pg = page_of(x.t0);
+    const bool row_ok = n < x.M;
+    const int rr = x.row0 + (row_ok ? n : 0), jq = rr / a.G, p = x.L + jq;  // row of the kv-head group, its position
+    const size_t orow = (size_t)(x.q0 + jq) * a.Hq + x.h * a.G + rr % a.G;
+    f32x4 qf[NB];
 #pragma unroll
-    for (int e = 0; e < 4; e++) s_o[wv][e][lane] = o[e];
-    if (lane == 0) {
-        s_ml[wv][0] = m;
-        s_ml[wv][1] = l;
+    for (int b = 0; b < NB; b++) {
+        const int d = 16 * b + 4 * q;
+        qf[b] = row_ok && d < HD ? *(const f32x4*)((const float*)a.q + orow * HD + d) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    f32x4 o[DG * 4];
+#pragma unroll
+    for (int d = 0; d < DG * 4; d++) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.0f;
+    for (int t = x.t0; t < x.t1; t++) {
+        const int s0 = list_tile(x.list, t) * kTile + 16 * w;
+        const int next = t + 1 < x.t1 ? page_of(t + 1) : -1;
+        auto row_at = [&](int page, int key) {
+            return ((((size_t)page * a.Hkv + x.h) << a.log2P) + ((s0 + key) & ((1 << a.log2P) - 1))) * HD;
+        };
+        f32x4 kf[NB], vf[4][DG];
+        const float* kp = (const float*)a.kc + row_at(max(pg, 0), n);
+#pragma unroll
+        for (int b = 0; b < NB; b++) {
+            const int d = 16 * b + 4 * q;
+            kf[b] = pg >= 0 && d < HD ? *(const f32x4*)(kp + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        int vpg[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            vpg[e] = __shfl(pg, 4 * q + e, 64);
+            const float* vp = (const float*)a.vc + row_at(max(vpg[e], 0), 4 * q + e);
+#pragma unroll
+            for (int g = 0; g < DG; g++) {
+                const int d = 64 * g + 4 * n;
+                vf[e][g] = vpg[e] >= 0 && d < HD ? *(const f32x4*)(vp + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+        const bool any = __any(pg >= 0);
+        pg = next;
+        if (!any) continue;
+        f32x4 s = {0.f, 0.f, 0.f, 0.f}, s2 = s;  // two chains
+#pragma unroll
+        for (int b = 0; b < NB; b++)
+#pragma unroll
+            for (int c = 0; c < 4; c += 2) {
+                s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][c], qf[b][c], s, 0, 0, 0);
+                s2 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][c + 1], qf[b][c + 1], s2, 0, 0, 0);
+            }
+        // keys s0 + 4 q + e of row n
+        float mx = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const int key = s0 + 4 * q + e;
+            const bool ok = (vpg[e] >= 0) & (key <= p) & ((key < a.sinks) | (key > p - a.window));
+            s[e] = ok ? (s[e] + s2[e]) * a.scale_log2 : -INFINITY;
+            mx = fmaxf(mx, s[e]);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.0f : m_new;
+        const float alpha = m == -INFINITY ? (l != 0.0f ? 1.0f : 0.0f) : exp2f(m - m_new);
+        m = m_new;
+        float sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            s[e] = exp2f(s[e] - ref);
+            sum += s[e];
+        }
+        l = l * alpha + sum;
+#pragma unroll
+        for (int d = 0; d < DG * 4; d++) o[d] *= alpha;
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+#pragma unroll
+            for (int d = 0; d < DG * 4; d++)
+                o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e][d / 4][d % 4], s[e], o[d], 0, 0, 0);
+    }
+    // merge the waves' states; wave w finishes every fourth block of 16 dims
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    s_ml[w][0][lane] = m;
+    s_ml[w][1][lane] = l;
+#pragma unroll
+    for (int d = 0; d < DG * 4; d++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) s_o[w][d][e][lane] = o[d][e];
     __syncthreads();
-    if (wv != 0) return;
-    float M = -INFINITY, lt = 0.0f, ot[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int w = 0; w < 4; w++) M = fmaxf(M, s_ml[w][0]);
-    for (int w = 0; w < 4; w++) {
-        const float mw = s_ml[w][0], wt = mw == -INFINITY ? (s_ml[w][1] != 0.0f ? 1.0f : 0.0f) : expf(mw - M);
-        lt += s_ml[w][1] * wt;
+    float M = -INFINITY, lt = 0.0f, wt[NW];
 #pragma unroll
-        for (int e = 0; e < 4; e++) ot[e] += s_o[w][e][lane] * wt;
+    for (int y = 0; y < NW; y++) M = fmaxf(M, s_ml[y][0][lane]);
+#pragma unroll
+    for (int y = 0; y < NW; y++) {
+        const float my = s_ml[y][0][lane], ly = s_ml[y][1][lane];
+        // (a part whose scores are all NaN has no maximum, but its sum counts)
+        wt[y] = my == -INFINITY ? (ly != 0.0f ? 1.0f : 0.0f) : exp2f(my - M);
+        lt += ly * wt[y];
     }
     const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
-    T* op = (T*)a.out + ((size_t)row * a.Hq + head) * HD;
+    const bool whole = a.splits == 1 || x.t1 - x.t0 == x.list.nt;
+    const size_t prow = (size_t)x.sp * a.total_q * a.Hq + orow;
+    float* out = whole ? (float*)a.out + orow * HD : a.part_o + prow * HD;
+    float odd = 0.0f;  // NaN where a result is not finite
+    for (int y = w; y < DG * 4; y += NW) {  // dims 64 (y / 4) + 16 q + 4 (y % 4) + c
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int e = 0; e < 4; e++)
-        if (lane + 64 * e < HD) store1(op + lane + 64 * e, ot[e] * inv);
-    if (a.lse && lane == 0) a.lse[(size_t)row * a.Hq + head] = lt == 0.0f ? -INFINITY : M + logf(lt);
+        for (int c = 0; c < 4; c++)
+#pragma unroll
+            for (int z = 0; z < NW; z++) v[c] += s_o[z][y / 4 * 4 + c][y % 4][lane] * wt[z];
+        const int d = 64 * (y / 4) + 16 * q + 4 * (y % 4);
+        if (row_ok && d < HD) {
+            *(f32x4*)(out + d) = v * inv;
+#pragma unroll
+            for (int c = 0; c < 4; c++) odd = __builtin_fmaf(v[c], 0.0f, odd);
+        }
+    }
+    if (w == 0 && q == 0 && row_ok) {
+        const float lse2 = lt == 0.0f ? -INFINITY : M + log2f(lt);
+        if (!whole) a.part_lse[prow] = lse2;
+        else if (a.lse) a.lse[orow] = lse2 * kLn2;
+    }
+    if (__syncthreads_or(odd != odd) && w == 0)
+        redo_rows<float>(a, x.i, x.h, x.sp, x.row0, 0, x.M, x.q0, x.L, x.list, x.t0, x.t1, 0, HD);
 }
 
 // ---------------------------------------------------------------------------------
@@ -188,31 +362,6 @@ struct WindowLds {
     int32_t holes;  // a page that the list needs is missing
 };
 
-// The outputs of rows r0 .. r1-1 of a row block once more, one by one, by one wave: dims d0 .. d1-1. A value that is
-// not finite reaches every row of its tile (0 * inf), those too that do not see it, so the rows of a
-// wave that finds such a result are done again from the definition. (Scores have no such neighbours.)
-template <int HD>
-__device__ __noinline__ void redo_rows(WindowArgs a, int i, int h, int sp, int row0, int r0, int r1, int q0, int L,
-                                       KeyList list, int t0, int t1, int d0, int d1) {
-    const int lane = threadIdx.x & 63;
-    for (int r = r0; r < r1; r++) {
-        const int rr = row0 + r, jq = rr / a.G, head = h * a.G + rr % a.G;
-        const size_t orow = (size_t)(q0 + jq) * a.Hq + head;
-        float o[4], m, l;
-        wave_row<uint16_t>(a, (const uint16_t*)a.q + orow * HD, a.page_table + (size_t)i * a.maxp, h, L + jq, list, t0, t1, 1,
-                           m, l, o);
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const bool whole = a.splits == 1 || t1 - t0 == list.nt;
-        const size_t prow = (size_t)sp * a.total_q * a.Hq + orow;
-        for (int e = 0; e < HD / 64; e++) {
-            const int d = lane + 64 * e;
-            if (d < d0 || d >= d1) continue;
-            if (whole) ((uint16_t*)a.out)[orow * HD + d] = f2bf(o[e] * inv);
-            else a.part_o[prow * HD + d] = o[e] * inv;
-        }
-    }
-}
-
 // wait until at most min(newer, MAX) tiles of IPW loads each are outstanding
 template <int MAX, int IPW>
 __device__ inline void wait_tiles(int newer) {
@@ -226,9 +375,9 @@ __device__ inline void wait_tiles(int newer) {
 
 // One item, its waves divided into row groups of PARTS waves
 template <int HD, int NW, int NBUF, Pages PM, int PARTS>
-__device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, NW, NBUF>& lds, int i, int h, int sp,
-                                            int row0, int q0, int L, int M, int last, const KeyList& list, int t0,
-                                            int t1) {
+__device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, NW, NBUF>& lds, const Item& x) {
+    const int i = x.i, h = x.h, sp = x.sp, row0 = x.row0, q0 = x.q0, L = x.L, M = x.M, last = x.last, t0 = x.t0, t1 = x.t1;
+    const KeyList list = x.list;
     constexpr int CPR = HD / 8;             // 16-byte chunks per token row
     constexpr int TPS = 1024 / (HD * 2);    // tokens per 1 KB DMA segment
     constexpr int NSEG = kTile / TPS;       // segments per tensor per tile
@@ -625,37 +774,21 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
         }
     }
     if (__any(odd != odd))
-        redo_rows<HD>(a, i, h, sp, row0, rg * 32, min(M, rg * 32 + 32), q0, L, list, t0, t1, th * (HD / PARTS),
+        redo_rows<uint16_t>(a, i, h, sp, row0, rg * 32, min(M, rg * 32 + 32), q0, L, list, t0, t1, th * (HD / PARTS),
                       (th + 1) * (HD / PARTS));
 }
 
 template <int HD, int NW, int NBUF, Pages PM>
 __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
     __shared__ __attribute__((aligned(16))) WindowLds<HD, NW, NBUF> lds;
-    // neighbouring workgroups go to the XCDs in turn: each takes a run of (request, split, kv-head)s, whose heads
-    // share pages, and the row blocks of one follow each other
-    // (the quotients of vector divisions, back in scalar registers: the copies' addresses need them there)
-    auto scalar = [](unsigned x) { return __builtin_amdgcn_readfirstlane((int)x); };
-    const unsigned slot = blockIdx.x / 8;
-    const int ux = scalar(slot / (unsigned)a.nrb), rb = scalar(slot % (unsigned)a.nrb);
-    const unsigned unit = (blockIdx.x % 8) * (unsigned)a.per_xcd + (unsigned)ux;
-    if (ux >= a.per_xcd || unit >= (unsigned)a.R * (unsigned)a.splits * (unsigned)a.Hkv) return;
-    const int h = scalar(unit % (unsigned)a.Hkv), is = scalar(unit / (unsigned)a.Hkv);
-    const int sp = scalar((unsigned)is % (unsigned)a.splits), i = scalar((unsigned)is / (unsigned)a.splits);
-    const int row0 = rb * NW * 32;
-    int q0, k_i, kv_len;
-    if (!load_request(a, i, q0, k_i, kv_len)) return;
-    const int M = min(a.G * k_i - row0, NW * 32);
-    if (M <= 0) return;
-    const int L = kv_len - k_i, last = kv_len - 1;  // the first and the last row's position
-    const KeyList list = key_list(a.window, a.sinks, L, k_i);
-    const int t0 = sp * a.split_tiles, t1 = min(list.nt, t0 + a.split_tiles);
-    if (t0 >= t1) return;
-    if (M <= NW * 16) window_item<HD, NW, NBUF, PM, 2>(a, lds, i, h, sp, row0, q0, L, M, last, list, t0, t1);
-    else window_item<HD, NW, NBUF, PM, 1>(a, lds, i, h, sp, row0, q0, L, M, last, list, t0, t1);
+    Item x;
+    if (!find_item(a, NW * 32, x)) return;
+    if (x.M <= NW * 16) window_item<HD, NW, NBUF, PM, 2>(a, lds, x);
+    else window_item<HD, NW, NBUF, PM, 1>(a, lds, x);
 }
 
 // The splits of the divided lists: one thread per (row, 4 dims).
+template <typename T>
 __global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a) {
     const int SL = a.HD / 4, i = blockIdx.y;
     int q0, k_i, kv_len;
@@ -694,10 +827,7 @@ __global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a) {
         mx = bm;
     }
     const float inv = wsum == 0.0f ? 0.0f : 1.0f / wsum;
-    uint64_t pk = 0;
-#pragma unroll
-    for (int e = 0; e < 4; e++) pk |= (uint64_t)f2bf(acc[e] * inv) << (16 * e);
-    *(uint64_t*)((uint16_t*)a.out + orow * a.HD + sl * 4) = pk;
+    Vec4<T>::put((T*)a.out + orow * a.HD + sl * 4, acc * inv);
     if (a.lse && sl == 0) a.lse[orow] = wsum == 0.0f ? -INFINITY : (mx + __log2f(wsum)) * kLn2;
 }
 
@@ -744,10 +874,6 @@ hipError_t launch_window(const sv_window_desc& w, const WindowPlan& plan, const 
     a.per_xcd = (int)((units + 7) / 8);
     a.scale = d.sm_scale > 0.0f ? d.sm_scale : 1.0f / sqrtf((float)d.head_dim);
     a.scale_log2 = a.scale * kLog2e;
-    if (d.dtype == SV_F32) {
-        hipLaunchKernelGGL(window_rows_kernel<float>, dim3(d.total_q_max * d.num_q_heads), dim3(256), 0, stream, a);
-        return hipGetLastError();
-    }
     const dim3 grid(8 * a.per_xcd * plan.row_blocks);
 #define SV_WINDOW(HD, NW, NB, PM) \
     hipLaunchKernelGGL((window_bf16_kernel<HD, NW, NB, Pages::PM>), grid, dim3(NW * 64), 0, stream, a)
@@ -755,7 +881,11 @@ hipError_t launch_window(const sv_window_desc& w, const WindowPlan& plan, const 
     if (d.page_size >= kTile) SV_WINDOW(HD, NW, NB, kTile); \
     else if (d.page_size >= 512 / HD) SV_WINDOW(HD, NW, NB, kSegment); \
     else SV_WINDOW(HD, NW, NB, kLane)
-    if (plan.waves == 4) {
+    if (d.dtype == SV_F32) {
+        if (d.head_dim <= 64) hipLaunchKernelGGL((window_f32_kernel<1>), grid, dim3(256), 0, stream, a);
+        else if (d.head_dim <= 128) hipLaunchKernelGGL((window_f32_kernel<2>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((window_f32_kernel<4>), grid, dim3(256), 0, stream, a);
+    } else if (plan.waves == 4) {
         if (d.head_dim == 128) { SV_WINDOW_PAGES(128, 4, 2); }
         else { SV_WINDOW_PAGES(64, 4, 4); }
     } else {
@@ -767,7 +897,9 @@ hipError_t launch_window(const sv_window_desc& w, const WindowPlan& plan, const 
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.splits == 1) return e;
     const long long slices = (long long)d.block * d.num_q_heads * (d.head_dim / 4);
-    hipLaunchKernelGGL(window_merge_kernel, dim3((unsigned)((slices + 255) / 256), d.num_reqs), dim3(256), 0, stream, a);
+    const dim3 mgrid((unsigned)((slices + 255) / 256), d.num_reqs);
+    if (d.dtype == SV_F32) hipLaunchKernelGGL(window_merge_kernel<float>, mgrid, dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL(window_merge_kernel<uint16_t>, mgrid, dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

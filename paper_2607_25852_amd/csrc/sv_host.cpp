@@ -255,12 +255,10 @@ sv_status check_window(const sv_window_desc* d) {
     if (st != SV_OK) return st;
     if (d->window < 1) return fail(SV_ERR_INVALID_ARG, "sv_window_attn: window %d < 1", d->window);
     if (d->sinks < 0) return fail(SV_ERR_INVALID_ARG, "sv_window_attn: sinks %d < 0", d->sinks);
-    // one flat grid of 256-thread workgroups: its work items must fit the 32-bit dispatch size
+    // one flat grid of at most 512-thread workgroups must fit the 32-bit dispatch size
     const WindowPlan p = plan_window(*d);
-    const long long groups = d->attn.dtype == SV_F32
-                                 ? (long long)d->attn.total_q_max * d->attn.num_q_heads
-                                 : ((long long)d->attn.num_reqs * p.splits * d->attn.num_kv_heads + 7) * p.row_blocks;
-    if (groups > (1 << 24) - 1)
+    const long long groups = ((long long)d->attn.num_reqs * p.splits * d->attn.num_kv_heads + 7) * p.row_blocks;
+    if (groups > (1 << 23) - 1)
         return fail(SV_ERR_UNSUPPORTED, "sv_window_attn: %lld work items exceed one launch", groups);
     return SV_OK;
 }
@@ -336,17 +334,21 @@ WindowPlan plan_window(const sv_window_desc& w) {
     const sv_attn_desc& d = w.attn;
     WindowPlan p{};
     const long long rows = (long long)(d.num_q_heads / d.num_kv_heads) * d.block;
-    p.splits = 1;
-    p.split_tiles = 0x7FFFFFFF;
-    if (d.dtype == SV_F32) return p;
-    p.waves = rows <= 128 ? 4 : 8;
-    p.row_blocks = (int)((rows + 32 * p.waves - 1) / (32 * p.waves));
+    // bf16: 32 rows per wave. fp32: all 16 rows of a block in each of four waves.
+    p.waves = d.dtype == SV_F32 || rows <= 128 ? 4 : 8;
+    p.block_rows = d.dtype == SV_F32 ? 16 : 32 * p.waves;
+    p.row_blocks = (int)((rows + p.block_rows - 1) / p.block_rows);
     constexpr int T = kWindowTile;
     const long long tiles = longest_list(w.window, w.sinks, d.block, d.max_kv_len);
     const long long units = (long long)d.num_reqs * d.num_kv_heads * p.row_blocks;
+    // Lists are divided where the units alone leave compute units idle: into about 512 items (two workgroups per
+    // compute unit), of at least 4 tiles (fp32: 2). A divided list costs a second kernel (about 5 us). bf16,
+    // windows of 1024: 128 units of 128 rows take 30 us divided and 38 us whole, 256 units 43 and 37 us, 216
+    // units of 64-wide heads 28 and 22 us; items of 2 tiles take no less than of 4 (13.7 and 13.5 us for 32
+    // units of 8 rows). fp32, 64 units, windows of 128: items of 2 tiles 13 us, of 4 tiles 15 us.
     long long per = tiles;
     if (d.kv_split > 0) per = std::max<long long>(1, d.kv_split / T);
-    else if (units < 512) per = std::max<long long>(4, (tiles * units + 511) / 512);
+    else if (units < 192) per = std::max<long long>(d.dtype == SV_F32 ? 2 : 4, (tiles * units + 511) / 512);
     p.split_tiles = (int)std::min(per, tiles);
     p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
     if (p.splits > 1) {

@@ -60,8 +60,9 @@ struct CompactPlan {
     size_t chunk_live, move_of, ws_bytes;
 };
 struct WindowPlan {
-    int waves;        // waves per workgroup (bf16): 4 or 8, of 32 query rows each
-    int row_blocks;   // row blocks of waves * 32 rows per (request, kv-head)
+    int waves;        // waves per workgroup, 4 or 8
+    int block_rows;   // query rows per row block
+    int row_blocks;   // row blocks per (request, kv-head)
     int splits, split_tiles;  // splits of every key list, tiles of 64 keys of each
     size_t part_o_bytes, ws_bytes;
 };

@@ -83,16 +83,13 @@ int main() {
         if (sv::check_window(&w) != SV_OK) continue;
         plans++;
         const sv::WindowPlan p = sv::plan_window(w);
-        if (d.dtype == SV_F32) {
-            expect(p.ws_bytes == 0, "no workspace", n, 0, 0, 0);
-            continue;
-        }
         const long long most = sv::longest_list(w.window, w.sinks, d.block, d.max_kv_len);
         expect(p.splits >= 1 && p.split_tiles >= 1 && (long long)p.splits * p.split_tiles >= most &&
                    (p.splits - 1LL) * p.split_tiles < most,
                "splits cover the longest list, none is empty", p.splits, p.split_tiles, most, n);
         const long long rows = (long long)(d.num_q_heads / d.num_kv_heads) * d.block;
-        expect((long long)p.row_blocks * p.waves * 32 >= rows, "row blocks", p.row_blocks, p.waves, rows, n);
+        expect((long long)p.row_blocks * p.block_rows >= rows, "row blocks", p.row_blocks, p.block_rows, rows, n);
+        expect(d.dtype == SV_F32 || p.block_rows == 32 * p.waves, "rows of a block", p.block_rows, p.waves, n, 0);
         const size_t parts = (size_t)p.splits * d.total_q_max * d.num_q_heads;
         if (p.splits > 1)
             expect(p.part_o_bytes >= parts * d.head_dim * 4 && p.ws_bytes >= p.part_o_bytes + parts * 4 &&

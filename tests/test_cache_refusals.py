@@ -90,7 +90,7 @@ WINDOW = dict(R=4, total_q_max=64, block=16, Hq=32, Hkv=8, d=128, page_size=64, 
     (dict(Hq=30), 1, 0, INVALID, "multiple"), (dict(d=96), 1, 0, UNSUPPORTED, "head_dim"), (dict(block=17), 1, 0, INVALID, "block"),
     (dict(total_q_max=65), 1, 0, INVALID, "num_reqs*block"),
     (dict(R=65535, kv_split=64, max_kv_len=8192), 1 << 20, 0, UNSUPPORTED, "one launch"),
-    (dict(R=65535, total_q_max=1 << 19, dtype=B.SV_F32), 1, 0, UNSUPPORTED, "one launch"), (dict(kv_split=63), 1, 0, INVALID, "kv_split")])
+    (dict(R=65535, kv_split=64, max_kv_len=8192, dtype=B.SV_F32), 1 << 20, 0, UNSUPPORTED, "one launch"), (dict(kv_split=63), 1, 0, INVALID, "kv_split")])
 def test_window_descriptor(lib, kw, window, sinks, status, msg):
     d = B.window_desc(B.attn_desc(**{**WINDOW, **kw}), window, sinks)
     assert lib.sv_window_attn(ctypes.byref(d), *[fake(i) for i in range(9)], BIG, None) == status
