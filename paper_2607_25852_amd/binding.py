@@ -206,10 +206,10 @@ def _rows_ptr(t, stride: int, name: str) -> int:
     """Device pointer of rows [n, heads, d] that lie `stride` elements apart (0: dense)."""
     if isinstance(t, int):
         return t
-    heads, d = t.shape[1:]
-    want = stride or heads * d
-    if (t.shape[0] > 1 and t.stride(0) != want) or (heads > 1 and t.stride(1) != d) or t.stride(2) != 1:
-        raise ValueError(f"{name}: strides {tuple(t.stride())} are not those of rows {want} elements apart")
+    n, heads, d = t.shape
+    want, st = stride or heads * d, t.stride()
+    if st != (want, d, 1) and ((n > 1 and st[0] != want) or (heads > 1 and st[1] != d) or (d > 1 and st[2] != 1)):
+        raise ValueError(f"{name}: strides {st} are not those of rows {want} elements apart")
     return t.data_ptr()
 
 
@@ -217,7 +217,19 @@ def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    # (the handle alone: building a Stream object takes longer than many of the calls)
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _run(fn, desc, like, stream, *args):
+    """fn(desc, *args, stream) on the device of tensor `like`: its current stream unless one is given."""
+    import torch
+    dev = like.device.index if isinstance(like, torch.Tensor) else None
+    if dev is None or dev == torch.cuda.current_device():
+        _check(fn(ctypes.byref(desc), *args, _stream(stream)))
+        return
+    with torch.cuda.device(dev):
+        _check(fn(ctypes.byref(desc), *args, _stream(stream)))
 
 
 def _dtype_code(t) -> int:
@@ -441,11 +453,9 @@ def rope_append(desc: RopeDesc, q, k_new, v_new, positions, inv_freq, page_table
                 k_cache, v_cache, stream=None):
     """sv_rope_append: q, k_new, v_new [total_max, heads, d] may be parts of wider rows (desc's strides);
     inv_freq [rot_dim / 2] float64."""
-    st = load().sv_rope_append(ctypes.byref(desc), _rows_ptr(q, desc.q_stride, "q"),
-                               _rows_ptr(k_new, desc.k_stride, "k_new"), _rows_ptr(v_new, desc.v_stride, "v_new"),
-                               _ptr(positions), _ptr(inv_freq), _ptr(page_table), _ptr(qo_indptr), _ptr(ctx_lens),
-                               _ptr(q_out), _ptr(k_cache), _ptr(v_cache), _stream(stream))
-    _check(st)
+    _run(load().sv_rope_append, desc, q_out, stream, _rows_ptr(q, desc.q_stride, "q"),
+         _rows_ptr(k_new, desc.k_stride, "k_new"), _rows_ptr(v_new, desc.v_stride, "v_new"), _ptr(positions),
+         _ptr(inv_freq), _ptr(page_table), _ptr(qo_indptr), _ptr(ctx_lens), _ptr(q_out), _ptr(k_cache), _ptr(v_cache))
 
 
 # ------------------------------------------------------------------------------------
@@ -464,10 +474,8 @@ def window_attn_workspace_size(desc: WindowDesc) -> int:
 def window_attn(desc: WindowDesc, q, k_cache, v_cache, page_table, qo_indptr, kv_lens, out, lse=None, ws=None,
                 stream=None):
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = load().sv_window_attn(ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
-                               _ptr(qo_indptr), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(ws), nbytes,
-                               _stream(stream))
-    _check(st)
+    _run(load().sv_window_attn, desc, out, stream, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
+         _ptr(qo_indptr), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(ws), nbytes)
 
 
 # ------------------------------------------------------------------------------------
@@ -480,9 +488,8 @@ def pages_desc(R: int, max_pages_per_req: int, num_pages: int, page_size: int) -
 
 
 def fork_pages(desc: PagesDesc, rows_in: int, table_in, lens_in, parent, table_out, lens_out, ref, stream=None):
-    st = load().sv_fork_pages(ctypes.byref(desc), rows_in, _ptr(table_in), _ptr(lens_in), _ptr(parent),
-                              _ptr(table_out), _ptr(lens_out), _ptr(ref), _stream(stream))
-    _check(st)
+    _run(load().sv_fork_pages, desc, ref, stream, rows_in, _ptr(table_in), _ptr(lens_in), _ptr(parent), _ptr(table_out),
+         _ptr(lens_out), _ptr(ref))
 
 
 def reserve_pages_workspace_size(desc: PagesDesc) -> int:
@@ -492,16 +499,12 @@ def reserve_pages_workspace_size(desc: PagesDesc) -> int:
 def reserve_pages(desc: PagesDesc, page_table, ref, ctx_lens, new_lens, copy_src, copy_dst, copy_tokens, info,
                   ws=None, stream=None):
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = load().sv_reserve_pages(ctypes.byref(desc), _ptr(page_table), _ptr(ref), _ptr(ctx_lens), _ptr(new_lens),
-                                 _ptr(copy_src), _ptr(copy_dst), _ptr(copy_tokens), _ptr(info), _ptr(ws), nbytes,
-                                 _stream(stream))
-    _check(st)
+    _run(load().sv_reserve_pages, desc, ref, stream, _ptr(page_table), _ptr(ref), _ptr(ctx_lens), _ptr(new_lens),
+         _ptr(copy_src), _ptr(copy_dst), _ptr(copy_tokens), _ptr(info), _ptr(ws), nbytes)
 
 
 def release_pages(desc: PagesDesc, page_table, ref, lens, window: int = 0, sinks: int = 0, stream=None):
-    st = load().sv_release_pages(ctypes.byref(desc), window, sinks, _ptr(page_table), _ptr(ref), _ptr(lens),
-                                 _stream(stream))
-    _check(st)
+    _run(load().sv_release_pages, desc, ref, stream, window, sinks, _ptr(page_table), _ptr(ref), _ptr(lens))
 
 
 def compact_pages_workspace_size(desc: PagesDesc) -> int:
@@ -510,9 +513,8 @@ def compact_pages_workspace_size(desc: PagesDesc) -> int:
 
 def compact_pages(desc: PagesDesc, max_moves: int, page_table, ref, move_src, move_dst, info, ws=None, stream=None):
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = load().sv_compact_pages(ctypes.byref(desc), max_moves, _ptr(page_table), _ptr(ref), _ptr(move_src),
-                                 _ptr(move_dst), _ptr(info), _ptr(ws), nbytes, _stream(stream))
-    _check(st)
+    _run(load().sv_compact_pages, desc, ref, stream, max_moves, _ptr(page_table), _ptr(ref), _ptr(move_src),
+         _ptr(move_dst), _ptr(info), _ptr(ws), nbytes)
 
 
 def copy_desc(max_copies: int, layers: int, Hkv: int, d: int, page_size: int, num_pages: int, dtype: int,
@@ -525,6 +527,5 @@ def copy_desc(max_copies: int, layers: int, Hkv: int, d: int, page_size: int, nu
 
 def copy_pages(desc: CopyDesc, src, dst, count, k_cache, v_cache, tokens=None, stream=None):
     """sv_copy_pages: count is a device tensor of one int32 (reserve_pages: info[2:3], compact_pages: info[:1])."""
-    st = load().sv_copy_pages(ctypes.byref(desc), _ptr(src), _ptr(dst), _ptr(tokens), _ptr(count), _ptr(k_cache),
-                              _ptr(v_cache), _stream(stream))
-    _check(st)
+    _run(load().sv_copy_pages, desc, k_cache, stream, _ptr(src), _ptr(dst), _ptr(tokens), _ptr(count), _ptr(k_cache),
+         _ptr(v_cache))

@@ -33,6 +33,11 @@ __global__ __launch_bounds__(kWalkThreads) void reserve_assign_kernel(ReserveArg
     reserve_assign<kWalkThreads>(a, blockIdx.x, wsum);
 }
 
+__global__ __launch_bounds__(kWalkThreads) void reserve_alone_kernel(ReserveArgs a) {
+    __shared__ ReserveLds<kWalkThreads> lds;
+    reserve_alone<kWalkThreads>(a, lds);
+}
+
 __global__ __launch_bounds__(kWalkThreads) void compact_count_kernel(CompactArgs a) {
     __shared__ uint32_t wsum[kWalkThreads / 64];
     count_chunk<kWalkThreads>(a.ref, a.num_pages, blockIdx.x, true, a.chunk_live, wsum);
@@ -61,11 +66,14 @@ struct CopyArgs {
     unsigned pieces;     // pieces per page and cache
 };
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kCopyLoads = 4;                   // vectors in flight per thread
 constexpr unsigned kPiece = 256 * kCopyLoads;   // vectors per piece (16 KB)
 
-// Bound by HBM: every byte is read and written once. A workgroup walks (copy, layer, cache, piece)
-// items; the vectors of the live tokens alone are numbered, head after head.
+// Bound by HBM: every byte is read and written once, past the caches (3930 pages of 32 KB in two layers and two
+// caches, 1.03 GB: 209 us with ordinary loads and stores, 193 us so; a large plain copy runs at 4.9 TB/s). A workgroup
+// walks (copy, layer, cache, piece) items; the vectors of the live tokens alone are numbered, head
+// after head. Eight vectors per thread instead of four took 1.5 times as long.
 __global__ __launch_bounds__(256) void copy_pages_kernel(CopyArgs a) {
     const long long n = min(*a.count, a.max_copies);
     const long long per_copy = 2LL * a.layers * a.pieces;
@@ -82,19 +90,19 @@ __global__ __launch_bounds__(256) void copy_pages_kernel(CopyArgs a) {
         if (piece * kPiece >= nv) continue;
         char* base = (lt & 1 ? a.vc : a.kc) + (size_t)(lt >> 1) * a.layer_bytes;
         const size_t page_vecs = (size_t)head_vecs * a.heads;
-        const uint4* from = (const uint4*)base + (size_t)src * page_vecs;
-        uint4* to = (uint4*)base + (size_t)dst * page_vecs;
-        uint4 x[kCopyLoads];
+        const u32x4* from = (const u32x4*)base + (size_t)src * page_vecs;
+        u32x4* to = (u32x4*)base + (size_t)dst * page_vecs;
+        u32x4 x[kCopyLoads];
         unsigned at[kCopyLoads];
 #pragma unroll
         for (int k = 0; k < kCopyLoads; k++) {
             const unsigned v = v0 + 256 * k;
             at[k] = live == a.P ? v : v / head_live * head_vecs + v % head_live;
-            if (v < nv) x[k] = from[at[k]];
+            if (v < nv) x[k] = __builtin_nontemporal_load(from + at[k]);
         }
 #pragma unroll
         for (int k = 0; k < kCopyLoads; k++)
-            if (v0 + 256 * k < nv) to[at[k]] = x[k];
+            if (v0 + 256 * k < nv) __builtin_nontemporal_store(x[k], to + at[k]);
     }
 }
 
@@ -134,6 +142,10 @@ hipError_t launch_reserve(const sv_pages_desc& d, const ReservePlan& p, int32_t*
     const ReserveArgs a{table, ref, ctx, new_lens, copy_src, copy_dst, copy_tokens, info, d.num_reqs,
                         d.max_pages_per_req, d.num_pages, ilog2i(d.page_size), p.chunks, w + p.writers, w + p.last,
                         w + p.demand, w + p.copy_of, w + p.upto, w + p.copies, w + p.chunk_free};
+    if (p.alone) {
+        hipLaunchKernelGGL(reserve_alone_kernel, dim3(1), dim3(kWalkThreads), 0, stream, a);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(reserve_demand_kernel, dim3(1 + p.chunks), dim3(kWalkThreads), 0, stream, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -268,22 +268,27 @@ __device__ inline void sum_chunks(const int32_t* v, int n, int b, uint32_t* wsum
     block_scan<NT>(y, wsum, all);
 }
 
-// the free pages of chunk b to the demands of the requests that are served
+// with F free pages: the requests that are served and their demands; thread 0 writes info if asked to
 template <int NT>
-__device__ inline void reserve_assign(const ReserveArgs& a, int b, uint32_t* wsum) {
-    const int tid = threadIdx.x;
-    uint32_t base, F, served;
-    sum_chunks<NT>(a.chunk_free, a.chunks, b, wsum, base, F);
-    uint32_t n = 0;
-    for (int i = tid; i < a.R; i += NT) n += a.upto[i] <= (int)F;  // (non-decreasing)
+__device__ inline uint32_t reserve_served(const ReserveArgs& a, uint32_t F, bool report, uint32_t* wsum) {
+    uint32_t n = 0, served;
+    for (int i = threadIdx.x; i < a.R; i += NT) n += a.upto[i] <= (int)F;  // (non-decreasing)
     block_scan<NT>(n, wsum, served);
     const uint32_t S = served ? (uint32_t)a.upto[served - 1] : 0;
-    if (b == 0 && tid == 0) {
+    if (report && threadIdx.x == 0) {
         a.info[0] = (int)served;
         a.info[1] = (int)S;
         a.info[2] = served ? a.copies[served - 1] : 0;
         a.info[3] = (int)(F - S);
     }
+    return S;
+}
+
+// The free pages of chunk b, of which `base` lie before it, to the first S demands. Returns the free pages up to
+// its end (or to the last one taken).
+template <int NT>
+__device__ inline uint32_t reserve_chunk(const ReserveArgs& a, int b, uint32_t base, uint32_t S, uint32_t* wsum) {
+    const int tid = threadIdx.x;
     // pages 4 at a time per thread, in the order of their ids
     for (int k0 = 0; k0 < kPageChunk && base < S; k0 += 4 * NT) {
         const int p0 = b * kPageChunk + k0 + 4 * tid;
@@ -310,6 +315,29 @@ __device__ inline void reserve_assign(const ReserveArgs& a, int b, uint32_t* wsu
         }
         base += total;
     }
+    return base;
+}
+
+// the assignment by a workgroup per chunk
+template <int NT>
+__device__ inline void reserve_assign(const ReserveArgs& a, int b, uint32_t* wsum) {
+    uint32_t base, F;
+    sum_chunks<NT>(a.chunk_free, a.chunks, b, wsum, base, F);
+    const uint32_t S = reserve_served<NT>(a, F, b == 0, wsum);
+    reserve_chunk<NT>(a, b, base, S, wsum);
+}
+
+// All of it by one workgroup. The walk ends with the last page taken, the count needs all.
+template <int NT>
+__device__ inline void reserve_alone(const ReserveArgs& a, ReserveLds<NT>& lds) {
+    uint32_t n = 0, F;
+    for (int p = threadIdx.x; p < a.num_pages; p += NT) n += a.ref[p] == 0;
+    reserve_demands<NT>(a, lds);
+    block_scan<NT>(n, lds.wsum, F);
+    __syncthreads();  // (the demands are in memory)
+    const uint32_t S = reserve_served<NT>(a, F, true, lds.wsum);
+    uint32_t base = 0;
+    for (int b = 0; b < a.chunks && base < S; b++) base = reserve_chunk<NT>(a, b, base, S, lds.wsum);
 }
 
 // ---- compact -------------------------------------------------------------------------

@@ -53,6 +53,7 @@ struct AcceptPlan {
 constexpr int kPageChunkSize = 4096;  // pages per workgroup of the page calls
 struct ReservePlan {  // offsets in int32 words
     int chunks;
+    bool alone;  // one workgroup walks all pages
     size_t writers, last, demand, copy_of, upto, copies, chunk_free, ws_bytes;
 };
 struct CompactPlan {

@@ -98,7 +98,7 @@ struct Reserved {
     Words table, ref, src, dst, tokens, info;
 };
 
-Reserved reserve(const Pool& p) {
+Reserved reserve(const Pool& p, bool alone) {
     Reserved o{p.table, p.ref, Words(p.R, -7), Words(p.R, -7), Words(p.R, -7), Words(4, -7)};
     const int chunks = (p.pages + sv::kPageChunk - 1) / sv::kPageChunk;
     Words writers(p.pages, 99), last(p.pages, 99), demand(p.pages, -5), copy_of(p.pages, -5), upto(p.R), copies(p.R),
@@ -107,6 +107,10 @@ Reserved reserve(const Pool& p) {
                       o.tokens.data(), o.info.data(), p.R, p.maxp, p.pages, p.log2P, chunks, writers.data(),
                       last.data(), demand.data(), copy_of.data(), upto.data(), copies.data(), chunk_free.data()};
     auto lds = std::make_unique<sv::ReserveLds<NT>>();
+    if (alone) {
+        hosthip::run_workgroup(NT, [&] { sv::reserve_alone<NT>(a, *lds); });
+        return o;
+    }
     hosthip::run_workgroup(NT, [&] { sv::reserve_demands<NT>(a, *lds); });
     for (int b = 0; b < chunks; b++)
         hosthip::run_workgroup(NT, [&] { sv::count_chunk<NT>(a.ref, a.num_pages, b, false, a.chunk_free, lds->wsum); });
@@ -151,12 +155,14 @@ Reserved reserve_in_order(const Pool& p) {
 }
 
 void check_reserve(const Pool& p, bool garbage) {
-    const Reserved got = reserve(p);
-    if (garbage) return;
-    const Reserved ref = reserve_in_order(p);
-    expect(got.info == ref.info, "reserve: info");
-    expect(got.table == ref.table && got.ref == ref.ref, "reserve: table and counts");
-    expect(got.src == ref.src && got.dst == ref.dst && got.tokens == ref.tokens, "reserve: copies");
+    for (bool alone : {false, true}) {
+        const Reserved got = reserve(p, alone);
+        if (garbage) continue;
+        const Reserved ref = reserve_in_order(p);
+        expect(got.info == ref.info, "reserve: info");
+        expect(got.table == ref.table && got.ref == ref.ref, "reserve: table and counts");
+        expect(got.src == ref.src && got.dst == ref.dst && got.tokens == ref.tokens, "reserve: copies");
+    }
 }
 
 void check_compact(const Pool& p, bool garbage) {
