@@ -124,8 +124,8 @@ __device__ void wave_row(const WindowArgs& a, const T* qp, const int32_t* pt, in
 // not finite reaches every row of its tile (0 * inf), those too that do not see it, so the rows of a
 // wave that finds such a result are done again from the definition. (Scores have no such neighbours.)
 template <typename T>
-__device__ __noinline__ void redo_rows(WindowArgs a, int i, int h, int sp, int row0, int r0, int r1, int q0, int L,
-                                       KeyList list, int t0, int t1, int d0, int d1) {
+__device__ __forceinline__ void redo_rows(const WindowArgs& a, int i, int h, int sp, int row0, int r0, int r1, int q0, int L,
+                                          const KeyList& list, int t0, int t1, int d0, int d1) {
     const int lane = threadIdx.x & 63, HD = a.HD;
     for (int r = r0; r < r1; r++) {
         const int rr = row0 + r, jq = rr / a.G, head = h * a.G + rr % a.G;
@@ -466,8 +466,10 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
     auto find_pages = [&](int t, int c0) {
         const int32_t* ids = lds.pid + ((t - c0) << log2T);
         if constexpr (PM == Pages::kLane) {
+            int x = seg0 * TPS + lane / CPR;
+            asm volatile("" : "+v"(x));  // (the addresses of all segments, kept through the loop, would not fit the registers)
 #pragma unroll
-            for (int k = 0; k < IPW; k++) pgv[k] = ids[token(k) >> log2S];
+            for (int k = 0; k < IPW; k++) pgv[k] = ids[(x + k * TPS) >> log2S];
         } else if constexpr (PM == Pages::kSegment) {
             pgv[0] = ids[((seg0 + (lane & (IPW - 1))) * TPS) >> log2S];
         } else {
@@ -502,6 +504,8 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
                 for (int k = 0; k < IPW; k++) dma16s(voff[k % NV], base + k / NV * (NV * TPS * HD * 2), lbuf + 1024 * k);
             }
         } else {
+            int x = seg0 * TPS + lane / CPR;
+            if constexpr (PM == Pages::kLane) asm volatile("" : "+v"(x));
 #pragma unroll
             for (int k = 0; k < IPW; k++) {
                 const int s0 = tb + (seg0 + k) * TPS;
@@ -509,9 +513,10 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
                 if constexpr (PM == Pages::kLane) {
                     const char* src = cbase;
                     if (pgv[k] >= 0 && !skip)
-                        src += (unsigned)pgv[k] * page_bytes + head_bytes + (uint32_t)((tb + token(k)) & pmask) * (HD * 2) +
+                        src += (unsigned)pgv[k] * page_bytes + head_bytes + (uint32_t)((tb + x + k * TPS) & pmask) * (HD * 2) +
                                (voff[k % NV] - (uint32_t)(lane / CPR) * (HD * 2));
                     dma16(src, lbuf + 1024 * k);
+                    __builtin_amdgcn_sched_barrier(0);
                 } else {
                     const unsigned pg = max(__builtin_amdgcn_readlane(pgv[0], k), 0);
                     const char* base = cbase + pg * page_bytes + head_bytes + (uint32_t)(s0 & pmask) * (HD * 2);
@@ -585,8 +590,10 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
 #pragma unroll
                 for (int x = 0; x < NSB; x++)
 #pragma unroll
-                    for (int e = 0; e < 16; e++)
+                    for (int e = 0; e < 16; e++) {
                         s[x][e] = ids[(32 * (th + x) + 4 * half + 8 * (e >> 2) + (e & 3)) >> log2S] < 0 ? -INFINITY : s[x][e];
+                        if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (few at a time: registers)
+                    }
             }
         }
         // the row's maximum: lane-local, then across the lane halves; the running maximum moves only when a
@@ -734,34 +741,39 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
         l_tot = l_tot * a1 + l2 * a2;
         m_run = mm;
     }
+    // (the row's place once more, from a thread id that the compiler cannot relate to the one above: kept through the
+    // loop, it would cost registers there)
+    int tid2 = threadIdx.x;
+    asm volatile("" : "+v"(tid2));
+    const int r2 = row0 + min(rg * 32 + (tid2 & 31), M - 1), half2 = (tid2 >> 5) & 1;
+    const size_t orow = (size_t)(q0 + r2 / a.G) * a.Hq + h * a.G + r2 % a.G;
     if (active && row_ok) {
         const float inv = l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
-        const float lse2 = l_tot == 0.0f ? -INFINITY : m_run * a.scale_log2 + __log2f(l_tot);
-        const size_t orow = (size_t)(q0 + jq) * a.Hq + head;
         const bool whole = a.splits == 1 || t1 - t0 == list.nt;
-        const size_t prow = (size_t)sp * a.total_q * a.Hq + orow;
+        // dims 32 t + 8 g + 4 half .. + 3
+        auto each = [&](auto put) {
 #pragma unroll
-        for (int t = 0; t < DT; t++) {
-            if (PARTS == 2 && t / (DT / 2) != th) continue;
+            for (int t = 0; t < DT; t++) {
+                if (PARTS == 2 && t / (DT / 2) != th) continue;
 #pragma unroll
-            for (int g = 0; g < 4; g++) {
-                const int d0 = t * 32 + 8 * g + 4 * half;
-                if (whole) {
-                    bf16x4 v;
-#pragma unroll
-                    for (int e = 0; e < 4; e++) v[e] = (__bf16)(o[t][4 * g + e] * inv);
-                    *(bf16x4*)((uint16_t*)a.out + orow * HD + d0) = v;
-                } else {
+                for (int g = 0; g < 4; g++) {
                     f32x4 v;
 #pragma unroll
                     for (int e = 0; e < 4; e++) v[e] = o[t][4 * g + e] * inv;
-                    *(f32x4*)(a.part_o + prow * HD + d0) = v;
+                    put(t * 32 + 8 * g, v);
                 }
             }
-        }
-        if (half == 0 && th == 0) {
-            if (!whole) a.part_lse[prow] = lse2;
-            else if (a.lse) a.lse[orow] = lse2 * kLn2;
+        };
+        const float lse2 = l_tot == 0.0f ? -INFINITY : m_run * a.scale_log2 + __log2f(l_tot);
+        if (whole) {
+            uint16_t* out = (uint16_t*)a.out + orow * HD + 4 * half2;
+            each([&](int d, f32x4 v) { Vec4<uint16_t>::put(out + d, v); });
+            if (a.lse && half2 == 0 && th == 0) a.lse[orow] = lse2 * kLn2;
+        } else {
+            const size_t prow = (size_t)sp * a.total_q * a.Hq + orow;
+            float* out = a.part_o + prow * HD + 4 * half2;
+            each([&](int d, f32x4 v) { Vec4<float>::put(out + d, v); });
+            if (half2 == 0 && th == 0) a.part_lse[prow] = lse2;
         }
     }
     float odd = 0.0f;  // NaN where a result is not finite
