@@ -257,7 +257,7 @@ sv_status check_window(const sv_window_desc* d) {
     if (d->sinks < 0) return fail(SV_ERR_INVALID_ARG, "sv_window_attn: sinks %d < 0", d->sinks);
     // one flat grid of at most 512-thread workgroups must fit the 32-bit dispatch size
     const WindowPlan p = plan_window(*d);
-    const long long groups = ((long long)d->attn.num_reqs * p.splits * d->attn.num_kv_heads + 7) * p.row_blocks;
+    const long long groups = ((long long)d->attn.num_reqs * p.splits + 7) * d->attn.num_kv_heads * p.row_blocks;
     if (groups > (1 << 23) - 1)
         return fail(SV_ERR_UNSUPPORTED, "sv_window_attn: %lld work items exceed one launch", groups);
     return SV_OK;
@@ -354,6 +354,8 @@ WindowPlan plan_window(const sv_window_desc& w) {
     else if (units < 192) per = std::max<long long>(d.dtype == SV_F32 ? 2 : 4, (tiles * units + 511) / 512);
     p.split_tiles = (int)std::min(per, tiles);
     p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
+    // (where every XCD gets two (request, split)s at least, and the rows may differ)
+    p.by_rows = d.block > 1 && d.num_reqs <= 64 && (long long)d.num_reqs * p.splits >= 16;
     if (p.splits > 1) {
         const size_t n = (size_t)p.splits * d.total_q_max * d.num_q_heads;
         p.part_o_bytes = n * d.head_dim * sizeof(float);
