@@ -364,7 +364,8 @@ __global__ __launch_bounds__(256, DG == 4 ? 1 : 2) void window_f32_kernel(Window
 // A workgroup of NW waves takes one (request, split, kv-head, row block): up to NW * 32 query rows of the
 // kv-head group (row r: position j = r / G, head r % G) against the split's tiles of 64 keys. Where the rows
 // fill half of the waves or less, two waves share 32 rows and take the halves of every tile
-// (PARTS = 2), else a wave takes both halves. As in attn.hip, S^T = K Q^T puts
+// (PARTS = 2), else a wave takes both halves; up to 32 rows are shared by all four waves, which take two tiles
+// at a time (PARTS = 4). As in attn.hip, S^T = K Q^T puts
 // the scores of a query row into one lane pair, and P^T is then in the operand layout of
 // O^T = V^T P^T, with V read transposed from LDS. K and V tiles come through the page table into an LDS
 // ring by direct loads while earlier tiles are multiplied; the parts of a row are merged at the end.
@@ -381,7 +382,7 @@ struct WindowLds {
             uint16_t k[NBUF][kTile * HD];  // [buffer][token * HD + d], swizzled (attn_tile.h)
             uint16_t v[NBUF][kTile * HD];
         };
-        float park[NW * HD * 16];  // half of the waves' partial outputs
+        float park[NW * HD * 32];  // the waves' partial outputs
     };
     float ml[NW][2][64];
     int32_t pid[kPageSlots];
@@ -432,6 +433,10 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
     if (tid == 0) lds.holes = 0;
 
     const int rg = w / PARTS, th = w % PARTS;
+    // with PARTS = 4 a step takes two tiles: the wave's tile of the step, and its half of that tile
+    constexpr int STEP = PARTS == 4 ? 2 : 1;
+    static_assert(NBUF % STEP == 0, "the tiles of a step are neighbours in the ring");
+    const int dt = PARTS == 4 ? th >> 1 : 0, hh = PARTS == 4 ? th & 1 : th;
     const int r = rg * 32 + (lane & 31), half = lane >> 5;
     const bool row_ok = r < M;
     const int rr = row0 + (row_ok ? r : 0);  // row within the request's kv-head group
@@ -448,7 +453,7 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
 #pragma unroll
             for (int t = 0; t < DT; t++) {
                 const int dd = 32 * t + 16 * (g & 1) + 4 * (jl & 3);
-                vofs[qh][t] = (th * 32 * HD + tl * HD + (((dd >> 3) ^ (swz(tl) & (CPR - 1))) << 3) + (dd & 7)) * 2;
+                vofs[qh][t] = (hh * 32 * HD + tl * HD + (((dd >> 3) ^ (swz(tl) & (CPR - 1))) << 3) + (dd & 7)) * 2;
             }
         }
     }
@@ -488,8 +493,8 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
     // The page ids of a tile are read from LDS one tile before its copies are issued: lane k has that of segment
     // k (kLane: every lane has its tokens'), so the look-up's latency is off the path.
     constexpr int NPG = PM == Pages::kLane ? IPW : 1;
-    int pgv[NPG];
-    auto find_pages = [&](int t, int c0) {
+    int pgs[STEP][NPG];
+    auto find_pages = [&](int t, int c0, int (&pgv)[NPG]) {
         const int32_t* ids = lds.pid + ((t - c0) << log2T);
         if constexpr (PM == Pages::kLane) {
             int x = seg0 * TPS + lane / CPR;
@@ -510,7 +515,7 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
     // Segments that no row sees are not fetched from memory: the first one of the cache is read again in
     // their place (which keeps the count of loads per tile).
     auto dead = [&](int s0, int s1) { return (s0 > last) | ((s0 >= a.sinks) & (s1 <= L - a.window)); };
-    auto issue_tile = [&](int t) {
+    auto issue_tile = [&](int t, const int (&pgv)[NPG]) {
         const int tb = list_tile(list, t) * kTile;
         const bool edge = tile_edge(tb) != 0;
         const uint32_t lbuf = my_ring + (uint32_t)(ibuf * kTile * HD * 2);
@@ -571,11 +576,11 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
     uint32_t kofs[KK];
 #pragma unroll
     for (int j = 0; j < KK; j++)
-        kofs[j] = (uint32_t)((th * 32 + (lane & 31)) * HD + (((2 * j + half) ^ (swz(lane & 31) & (CPR - 1))) << 3)) * 2u;
+        kofs[j] = (uint32_t)((hh * 32 + (lane & 31)) * HD + (((2 * j + half) ^ (swz(lane & 31) & (CPR - 1))) << 3)) * 2u;
     // One online-softmax step: this wave's NSB halves (32 keys each) of a tile. The products' operands are read
     // from LDS a few products ahead; the scheduling barriers keep that order. With two halves, the
     // exponents of the second are computed between the first half's products with V.
-    constexpr int NSB = 2 / PARTS;
+    constexpr int NSB = PARTS == 1 ? 2 : 1;
     auto compute_tile = [&](int t, int c0, int buf, int edge) {
         const char* kt = (const char*)lds.k[buf];
         const char* vt = (const char*)lds.v[buf];
@@ -602,7 +607,7 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
         }
         // register e of half x holds key base + 32 x + y, y = 8 (e / 4) + e % 4
         if (edge) {
-            const int base = list_tile(list, t) * kTile + 32 * th + 4 * half;
+            const int base = list_tile(list, t) * kTile + 32 * hh + 4 * half;
             const int hi = p - base, past = p - a.window - base, first = a.sinks - base;
 #pragma unroll
             for (int x = 0; x < NSB; x++)
@@ -617,7 +622,7 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
                 for (int x = 0; x < NSB; x++)
 #pragma unroll
                     for (int e = 0; e < 16; e++) {
-                        s[x][e] = ids[(32 * (th + x) + 4 * half + 8 * (e >> 2) + (e & 3)) >> log2S] < 0 ? -INFINITY : s[x][e];
+                        s[x][e] = ids[(32 * (hh + x) + 4 * half + 8 * (e >> 2) + (e & 3)) >> log2S] < 0 ? -INFINITY : s[x][e];
                         if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (few at a time: registers)
                     }
             }
@@ -698,7 +703,7 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
     };
 
     // Tile t: wait for its copies (and only those), barrier (tile visible; the buffer that the next copies
-    // fill no longer read), start those of tile t + NBUF - 1, multiply. (The first NBUF start together.)
+    // fill no longer read), start those of the tiles that they take, multiply. (The first NBUF start together.)
     const bool active = rg * 32 < M;
     int buf = 0;
     for (int c0 = t0; c0 < t1; c0 += chunk_tiles) {
@@ -711,62 +716,86 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
 #pragma unroll
         for (int x = 0; x < NBUF; x++)
             if (c0 + x < c1) {
-                find_pages(c0 + x, c0);
-                issue_tile(c0 + x);
+                find_pages(c0 + x, c0, pgs[x % STEP]);
+                issue_tile(c0 + x, pgs[x % STEP]);
             }
-        if (c0 + NBUF < c1) find_pages(c0 + NBUF, c0);
-        for (int t = c0; t < c1; t++) {
-            const int edge = tile_edge(list_tile(list, t) * kTile);
-            wait_tiles<NBUF - 1, IPW>(min(t == c0 ? NBUF - 1 : NBUF - 2, c1 - 1 - t));
-            if (edge != 0 && my_tensor == 1) clean_tile(t, c0, buf, edge);
+#pragma unroll
+        for (int x = 0; x < STEP; x++)
+            if (c0 + NBUF + x < c1) find_pages(c0 + NBUF + x, c0, pgs[x]);
+        for (int t = c0; t < c1; t += STEP) {
+            int edge[STEP];
+#pragma unroll
+            for (int x = 0; x < STEP; x++) edge[x] = t + x < c1 ? tile_edge(list_tile(list, t + x) * kTile) : 0;
+            const int end = min(t + STEP, c1);  // tiles issued after these: up to the ring's length ahead of the last step
+            wait_tiles<NBUF - STEP, IPW>(min(c1, (t == c0 ? t : t - STEP) + NBUF) - end);
+            if (my_tensor == 1) {
+#pragma unroll
+                for (int x = 0; x < STEP; x++)
+                    if (edge[x] != 0) clean_tile(t + x, c0, buf + x, edge[x]);
+            }
             __syncthreads();
-            if (t > c0 && t + NBUF - 1 < c1) {
-                issue_tile(t + NBUF - 1);
-                if (t + NBUF < c1) find_pages(t + NBUF, c0);
+            if (t > c0) {
+#pragma unroll
+                for (int x = 0; x < STEP; x++) {
+                    const int next = t + NBUF - STEP + x;
+                    if (next >= c1) break;
+                    issue_tile(next, pgs[x]);
+                    if (next + STEP < c1) find_pages(next + STEP, c0, pgs[x]);
+                }
             }
-            if (active) compute_tile(t, c0, buf, edge);
-            buf = buf + 1 == NBUF ? 0 : buf + 1;
+            if (active && t + dt < c1) compute_tile(t + dt, c0, buf + dt, STEP == 2 && dt ? edge[STEP - 1] : edge[0]);
+            buf = buf + STEP == NBUF ? 0 : buf + STEP;
         }
         ibuf = buf;
     }
 
-    // The parts of a row group hold the same (row, dim) elements in the same lanes and registers; each parks
-    // the d-tiles that the other one finishes in the ring.
+    // The parts of a row group hold the same (row, dim) elements in the same lanes and registers; each finishes DO of
+    // the d-tiles and parks the others in the ring.
     float l_tot = l_run + __shfl_xor(l_run, 32, 64);
-    if constexpr (PARTS == 2) {
+    constexpr int DO = DT >= PARTS ? DT / PARTS : 1;
+    if constexpr (PARTS > 1) {
         __syncthreads();  // (the ring is free)
         f32x4* park = (f32x4*)lds.park + lane;
         lds.ml[w][0][lane] = m_run;
         lds.ml[w][1][lane] = l_tot;
-        auto put = [&](int from) {
 #pragma unroll
-            for (int t = 0; t < DT / 2; t++)
+        for (int t = 0; t < DT; t++) {
+            if (t / DO == th) continue;
 #pragma unroll
-                for (int g = 0; g < 4; g++)
-                    park[((w * (DT / 2) + t) * 4 + g) * 64] = f32x4{o[from + t][4 * g], o[from + t][4 * g + 1],
-                                                                    o[from + t][4 * g + 2], o[from + t][4 * g + 3]};
-        };
-        if (th) put(0);
-        else put(DT / 2);
+            for (int g = 0; g < 4; g++)
+                park[((w * DT + t) * 4 + g) * 64] = f32x4{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]};
+        }
         __syncthreads();
-        const float m2 = lds.ml[w ^ 1][0][lane], l2 = lds.ml[w ^ 1][1][lane], mm = fmaxf(m_run, m2);
-        // (a part whose scores are all NaN has no maximum, but its sum counts)
-        const float a1 = m_run == -INFINITY ? (l_tot != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m_run - mm);
-        const float a2 = m2 == -INFINITY ? (l2 != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(m2 - mm);
-        auto get = [&](int from) {
+        float mm = m_run, wt[PARTS];
 #pragma unroll
-            for (int t = 0; t < DT / 2; t++)
+        for (int x = 0; x < PARTS; x++) mm = fmaxf(mm, lds.ml[rg * PARTS + x][0][lane]);
+        l_tot = 0.0f;
+#pragma unroll
+        for (int x = 0; x < PARTS; x++) {
+            const float mx = lds.ml[rg * PARTS + x][0][lane], lx = lds.ml[rg * PARTS + x][1][lane];
+            // (a part whose scores are all NaN has no maximum, but its sum counts)
+            wt[x] = mx == -INFINITY ? (lx != 0.0f ? 1.0f : 0.0f) : __builtin_amdgcn_exp2f(mx - mm);
+            l_tot += lx * wt[x];
+        }
+        m_run = mm;
+#pragma unroll
+        for (int t = 0; t < DT; t++) {
+            if (t / DO != th) continue;
+            float mine = wt[0];
+#pragma unroll
+            for (int x = 1; x < PARTS; x++) mine = x == th ? wt[x] : mine;
+            o[t] *= mine;
+#pragma unroll
+            for (int x = 0; x < PARTS; x++) {
+                if (x == th) continue;
 #pragma unroll
                 for (int g = 0; g < 4; g++) {
-                    const f32x4 v = park[(((w ^ 1) * (DT / 2) + t) * 4 + g) * 64];
+                    const f32x4 v = park[(((rg * PARTS + x) * DT + t) * 4 + g) * 64];
 #pragma unroll
-                    for (int e = 0; e < 4; e++) o[from + t][4 * g + e] = o[from + t][4 * g + e] * a1 + v[e] * a2;
+                    for (int e = 0; e < 4; e++) o[t][4 * g + e] += v[e] * wt[x];
                 }
-        };
-        if (th) get(DT / 2);
-        else get(0);
-        l_tot = l_tot * a1 + l2 * a2;
-        m_run = mm;
+            }
+        }
     }
     // (the row's place once more, from a thread id that the compiler cannot relate to the one above: kept through the
     // loop, it would cost registers there)
@@ -781,7 +810,7 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
         auto each = [&](auto put) {
 #pragma unroll
             for (int t = 0; t < DT; t++) {
-                if (PARTS == 2 && t / (DT / 2) != th) continue;
+                if (PARTS > 1 && t / DO != th) continue;
 #pragma unroll
                 for (int g = 0; g < 4; g++) {
                     f32x4 v;
@@ -808,22 +837,24 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
         if (m_run != -INFINITY && !(l_tot > 0.0f && l_tot < INFINITY)) odd = NAN;
 #pragma unroll
         for (int t = 0; t < DT; t++) {
-            if (PARTS == 2 && t / (DT / 2) != th) continue;
+            if (PARTS > 1 && t / DO != th) continue;
 #pragma unroll
             for (int e = 0; e < 16; e++) odd = __builtin_fmaf(o[t][e], 0.0f, odd);
         }
     }
     if (__any(odd != odd))
-        redo_rows<uint16_t>(a, i, h, sp, row0, rg * 32, min(M, rg * 32 + 32), q0, L, list, t0, t1, th * (HD / PARTS),
-                      (th + 1) * (HD / PARTS));
+        redo_rows<uint16_t>(a, i, h, sp, row0, rg * 32, min(M, rg * 32 + 32), q0, L, list, t0, t1, PARTS > 1 ? th * DO * 32 : 0,
+                      PARTS > 1 ? min((th + 1) * DO * 32, HD) : HD);
 }
 
-template <int HD, int NW, int NBUF, Pages PM>
+// FEW: at most 32 rows (of every request)
+template <int HD, int NW, int NBUF, Pages PM, bool FEW>
 __global__ __launch_bounds__(NW * 64, 2) void window_bf16_kernel(WindowArgs a) {
     __shared__ __attribute__((aligned(16))) WindowLds<HD, NW, NBUF> lds;
     Item x;
-    if (!find_item(a, NW * 32, x)) return;
-    if (x.M <= NW * 16) window_item<HD, NW, NBUF, PM, 2>(a, lds, x);
+    if (!find_item(a, FEW ? 32 : NW * 32, x)) return;
+    if constexpr (FEW) window_item<HD, NW, NBUF, PM, 4>(a, lds, x);
+    else if (x.M <= NW * 16) window_item<HD, NW, NBUF, PM, 2>(a, lds, x);
     else window_item<HD, NW, NBUF, PM, 1>(a, lds, x);
 }
 
@@ -916,22 +947,25 @@ hipError_t launch_window(const sv_window_desc& w, const WindowPlan& plan, const 
     a.scale = d.sm_scale > 0.0f ? d.sm_scale : 1.0f / sqrtf((float)d.head_dim);
     a.scale_log2 = a.scale * kLog2e;
     const dim3 grid(8 * a.per_xcd * plan.row_blocks);
-#define SV_WINDOW(HD, NW, NB, PM) \
-    hipLaunchKernelGGL((window_bf16_kernel<HD, NW, NB, Pages::PM>), grid, dim3(NW * 64), 0, stream, a)
-#define SV_WINDOW_PAGES(HD, NW, NB) \
-    if (d.page_size >= kTile) SV_WINDOW(HD, NW, NB, kTile); \
-    else if (d.page_size >= 512 / HD) SV_WINDOW(HD, NW, NB, kSegment); \
-    else SV_WINDOW(HD, NW, NB, kLane)
+#define SV_WINDOW(HD, NW, NB, PM, FEW) \
+    hipLaunchKernelGGL((window_bf16_kernel<HD, NW, NB, Pages::PM, FEW>), grid, dim3(NW * 64), 0, stream, a)
+#define SV_WINDOW_PAGES(HD, NW, NB, FEW) \
+    if (d.page_size >= kTile) SV_WINDOW(HD, NW, NB, kTile, FEW); \
+    else if (d.page_size >= 512 / HD) SV_WINDOW(HD, NW, NB, kSegment, FEW); \
+    else SV_WINDOW(HD, NW, NB, kLane, FEW)
     if (d.dtype == SV_F32) {
         if (d.head_dim <= 64) hipLaunchKernelGGL((window_f32_kernel<1>), grid, dim3(256), 0, stream, a);
         else if (d.head_dim <= 128) hipLaunchKernelGGL((window_f32_kernel<2>), grid, dim3(256), 0, stream, a);
         else hipLaunchKernelGGL((window_f32_kernel<4>), grid, dim3(256), 0, stream, a);
+    } else if (plan.few) {
+        if (d.head_dim == 128) { SV_WINDOW_PAGES(128, 4, 4, true); }
+        else { SV_WINDOW_PAGES(64, 4, 4, true); }
     } else if (plan.waves == 4) {
-        if (d.head_dim == 128) { SV_WINDOW_PAGES(128, 4, 2); }
-        else { SV_WINDOW_PAGES(64, 4, 4); }
+        if (d.head_dim == 128) { SV_WINDOW_PAGES(128, 4, 2, false); }
+        else { SV_WINDOW_PAGES(64, 4, 4, false); }
     } else {
-        if (d.head_dim == 128) { SV_WINDOW_PAGES(128, 8, 4); }
-        else { SV_WINDOW_PAGES(64, 8, 4); }
+        if (d.head_dim == 128) { SV_WINDOW_PAGES(128, 8, 4, false); }
+        else { SV_WINDOW_PAGES(64, 8, 4, false); }
     }
 #undef SV_WINDOW_PAGES
 #undef SV_WINDOW

@@ -354,6 +354,11 @@ WindowPlan plan_window(const sv_window_desc& w) {
     else if (units < 192) per = std::max<long long>(d.dtype == SV_F32 ? 2 : 4, (tiles * units + 511) / 512);
     p.split_tiles = (int)std::min(per, tiles);
     p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
+    // All four waves on the same 32 rows, two tiles at a time: a step takes as long as one of two waves on one tile
+    // (27 requests of 8 positions and 64-wide heads 18.8 and 22.0 us). 128-wide heads need the LDS of a whole compute
+    // unit for it, which pays where every unit has one (192 units of 8 rows, windows of 1024: 26.9 and 29.7 us, 512
+    // units 55 and 48 us) and walks its whole list (32 units in 5 splits 14.2 and 13.8 us).
+    p.few = d.dtype == SV_BF16 && rows <= 32 && (d.head_dim == 64 || (units <= 256 && p.splits == 1));
     // Where the rows may differ, every XCD gets two (request, split)s at least and there is enough to do that the
     // order repays finding it (0.5 to 1 us: 3900 tiles in all lose 1 of 22 us, 9700 win 1 of 56)
     p.by_rows = d.block > 1 && d.num_reqs <= 64 && (long long)d.num_reqs * p.splits >= 16 && tiles * units >= 8192;

@@ -66,6 +66,7 @@ struct WindowPlan {
     int row_blocks;   // row blocks per (request, kv-head)
     int splits, split_tiles;  // splits of every key list, tiles of 64 keys of each
     bool by_rows;     // the requests with the most rows first
+    bool few;         // at most 32 rows, shared by the four waves
     size_t part_o_bytes, ws_bytes;
 };
 AttnPlan plan_attn(const sv_attn_desc& d);
