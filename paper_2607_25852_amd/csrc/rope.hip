@@ -83,8 +83,8 @@ __device__ inline void store1(float* p, float f) { *p = f; }
 __device__ inline void store1(uint16_t* p, float f) { *p = f2bf(f); }
 
 // grid (row, part of the row's tasks). VEC: a task turns the pairs of one chunk (adjacent dims) or of
-// two chunks (dims of either half), or copies a chunk; else it turns one pair, or copies one element. STREAM: the
-// rows are read past the caches. (Two tasks per thread in flight, the first ones under the row's angles and
+// two chunks (dims of either half), or copies a chunk; else it turns one pair, or copies one element. STREAM: rows
+// are read and written past the caches. (Two tasks per thread in flight, the first ones under the row's angles and
 // page, took 3.5 us instead of 3.2 for 4 rows and 53 instead of 48 for 14996.)
 template <typename T, bool ADJ, bool VEC, bool STREAM>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
@@ -136,6 +136,10 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
         if constexpr (STREAM) return __builtin_nontemporal_load((const u32x4*)p);
         else return *(const u32x4*)p;
     };
+    auto store = [](T* p, u32x4 x) {
+        if constexpr (STREAM) __builtin_nontemporal_store(x, (u32x4*)p);
+        else *(u32x4*)p = x;
+    };
     for (int t = blockIdx.y * 256 + tid; t < a.tasks; t += gridDim.y * 256) {
         const bool value = t >= heads * a.tasks_per_head;
         const int per = value ? d / N : a.tasks_per_head;
@@ -150,7 +154,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
                               : (T*)a.q_out + ((size_t)row * a.Hq + h) * d;
         if (value || c >= a.turns_per_head) {
             const int at = value ? c * N : 2 * half + (c - a.turns_per_head) * N;
-            if constexpr (VEC) *(u32x4*)(dst + at) = chunk(src + at);
+            if constexpr (VEC) store(dst + at, chunk(src + at));
             else dst[at] = src[at];
             continue;
         }
@@ -169,7 +173,7 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
                 const float u0 = x[e] * w.x - x[e + 1] * w.y, u1 = x[e + 1] * w.x + x[e] * w.y;
                 x[e] = u0, x[e + 1] = u1;
             }
-            *(u32x4*)(dst + c * N) = Chunk<T>::put(x);
+            store(dst + c * N, Chunk<T>::put(x));
         } else {
             float x[N], y[N];
             Chunk<T>::get(chunk(src + c * N), x);
@@ -180,8 +184,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
                 const float u0 = x[e] * w.x - y[e] * w.y, u1 = y[e] * w.x + x[e] * w.y;
                 x[e] = u0, y[e] = u1;
             }
-            *(u32x4*)(dst + c * N) = Chunk<T>::put(x);
-            *(u32x4*)(dst + half + c * N) = Chunk<T>::put(y);
+            store(dst + c * N, Chunk<T>::put(x));
+            store(dst + half + c * N, Chunk<T>::put(y));
         }
     }
 }
@@ -237,13 +241,14 @@ hipError_t launch_rope(const sv_rope_desc& d, const void* q, const void* k_new, 
     // a row is divided among workgroups where the rows alone are too few
     const int parts = std::max(1, std::min((a.tasks + 255) / 256, 2048 / d.total_max));
     const dim3 grid(d.total_max, parts);
-    // Rows of many megabytes come from memory and are not read again; fewer rows were just written and lie in the
-    // caches. 14996 rows (276 MB): 48 us past the caches, 55 us through them; 512 rows (21 MB): 6.5 and 5.9 us.
-    const bool stream_in = (size_t)d.total_max * (d.num_q_heads + 2 * d.num_kv_heads) * d.head_dim * esz > (size_t)64 << 20;
+    // Rows of many megabytes go past the caches both ways. 14996 rows (138 MB in, as much out): 47 us, through the caches
+    // 55 us from memory and 47 us where the rows still lie in the last-level cache; 7500 rows 26 us, 32 and 23 us. Fewer rows
+    // were just written and are about to be read: 512 rows 6.5 us past the caches, 5.9 us through them.
+    const bool past = (size_t)d.total_max * (d.num_q_heads + 2 * d.num_kv_heads) * d.head_dim * esz > (size_t)64 << 20;
 #define SV_ROPE(T, ADJ, VEC, S) hipLaunchKernelGGL((rope_kernel<T, ADJ, VEC, S>), grid, dim3(256), 0, stream, a)
 #define SV_ROPE_VEC(T, ADJ) \
     if (!vec) SV_ROPE(T, ADJ, false, false); \
-    else if (stream_in) SV_ROPE(T, ADJ, true, true); \
+    else if (past) SV_ROPE(T, ADJ, true, true); \
     else SV_ROPE(T, ADJ, true, false)
 #define SV_ROPE_TYPE(T) \
     if (adj) { SV_ROPE_VEC(T, true); } \
