@@ -17,15 +17,30 @@ __device__ inline int load_counted(const int32_t* p) {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// sum of v over lanes 0 .. lane of the wave
+__device__ inline uint32_t wave_scan(uint32_t v) {
+#ifdef __AMDGCN__
+    // within rows of 16 lanes by 1, 2, 4, 8, then the last lane of a row (of two) to the rows after it
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);
+#else
+    for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t u = __shfl_up(v, off, 64);
+        if ((int)(threadIdx.x & 63) >= off) v += u;
+    }
+#endif
+    return v;
+}
+
 // sum of v over the threads before this one; total: over all. wsum: NT / 64 entries of LDS.
 template <int NT>
 __device__ inline uint32_t block_scan(uint32_t v, uint32_t* wsum, uint32_t& total) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    uint32_t incl = v;
-    for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t u = __shfl_up(incl, off, 64);
-        if (lane >= off) incl += u;
-    }
+    const uint32_t incl = wave_scan(v);
     __syncthreads();  // (wsum may still be read by an earlier scan)
     if (lane == 63) wsum[w] = incl;
     __syncthreads();
@@ -179,9 +194,11 @@ __device__ inline void reserve_demands(const ReserveArgs& a, ReserveLds<NT>& lds
         x.holders = (unsigned)x.page < (unsigned)a.num_pages ? max(a.ref[x.page], 1) : 0;
         return x;
     };
+    // each thread's first entry is read once (a round's batch rarely has more)
+    const Entry first = (uint32_t)tid < E ? entry(tid) : Entry{};
     bool any = false;
     for (uint32_t e = tid; e < E; e += NT) {
-        const Entry x = entry(e);
+        const Entry x = e < NT ? first : entry(e);
         if (x.holders > 1) {
             a.writers[x.page] = 0;
             a.last[x.page] = -1;
@@ -193,7 +210,7 @@ __device__ inline void reserve_demands(const ReserveArgs& a, ReserveLds<NT>& lds
     const bool shared = lds.shared != 0;
     if (shared) {
         for (uint32_t e = tid; e < E; e += NT) {
-            const Entry x = entry(e);
+            const Entry x = e < NT ? first : entry(e);
             if (x.holders > 1) {
                 atomicAdd(&a.writers[x.page], 1);
                 atomicMax(&a.last[x.page], (int)e);
@@ -207,7 +224,7 @@ __device__ inline void reserve_demands(const ReserveArgs& a, ReserveLds<NT>& lds
         bool want = false, copy = false;
         Entry x{};
         if (e < E) {
-            x = entry(e);
+            x = e < NT ? first : entry(e);
             want = x.holders == 0;
             if (x.holders > 1)
                 want = !(load_counted(&a.writers[x.page]) == x.holders && load_counted(&a.last[x.page]) == (int)e);
