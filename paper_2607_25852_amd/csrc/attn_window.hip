@@ -215,7 +215,7 @@ __device__ __forceinline__ bool find_item(const WindowArgs& a, int block_rows, I
 // Keys that no row sees are not loaded. Bound by the latency of a tile's loads (page, K and V) and by the chain of
 // its products (fp32 products run at a sixteenth of the bf16 rate). With 32 rows per wave (twice the
 // products per load, half the waves) 8 requests of 5 positions and windows of 512 took 26.8 us, with 16
-// rows 20.3 us.
+// rows 20.3 us; with the next tile's keys loaded ahead 21.7 instead of 20.7 us, 32 requests 47 instead of 43 us.
 template <int DG>
 __global__ __launch_bounds__(256, DG == 4 ? 1 : 2) void window_f32_kernel(WindowArgs a) {
     constexpr int NW = 4, NB = 4 * DG;  // waves; 16-dim blocks of the scores' sum

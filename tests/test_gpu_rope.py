@@ -124,6 +124,37 @@ def test_prompts_and_many_requests(dev):
     check(make(dev, 5, k, rng.integers(0, 9, 4200), 1, 1, 8, 8, "f32", (4,)))
 
 
+@pytest.mark.parametrize("dtype,n,Hq,Hkv,d,pairing", [("bf16", 5601, 30, 9, 128, "halves"),
+                                                      ("f32", 3500, 38, 1, 128, "adjacent")])
+def test_large_batches(dev, dtype, n, Hq, Hkv, d, pairing):
+    """More than 64 MB of rows are read and written past the caches: the same bits as the rows in small batches."""
+    from paper_2607_25852_amd import binding as B
+    torch, page = dev, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    dt, code = (torch.bfloat16, B.SV_BF16) if dtype == "bf16" else (torch.float32, B.SV_F32)
+    q, kn, vn = (torch.randn((n, h, d), generator=g, device="cuda").to(dt) for h in (Hq, Hkv, Hkv))
+    assert sum(x.numel() * x.element_size() for x in (q, kn, vn)) > 64 << 20
+    pos = torch.randint(0, 9000, (2, n), generator=g, device="cuda", dtype=torch.int32)
+    freq = 10000.0 ** (-torch.arange(64, dtype=torch.float64, device="cuda") / 64)
+    cols = -(-(n + 5) // page)
+    table = torch.randperm(cols + 3, generator=g, device="cuda")[:cols].to(torch.int32)[None].contiguous()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    code_of = dict(order=B.SV_ROPE_BLOCKS, pairing=B.SV_ROPE_ADJACENT if pairing == "adjacent" else B.SV_ROPE_HALVES)
+    res = []
+    for step in (n, 700):
+        say("rope large", dtype, pairing, step)
+        out = torch.zeros_like(q)
+        kc, vc = (torch.zeros((cols + 3, Hkv, page, d), dtype=dt, device="cuda") for _ in range(2))
+        for r in range(0, n, step):
+            m = min(step, n - r)
+            desc = B.rope_desc(1, m, Hq, Hkv, d, (40, 24), page, cols, cols + 3, code, **code_of)
+            B.rope_append(desc, q[r:r + m], kn[r:r + m], vn[r:r + m], pos[:, r:r + m].contiguous(), freq, table, i32(0, m),
+                          i32(5 + r), out[r:r + m], kc, vc)
+        res.append((out, kc, vc))
+    for x, y in zip(*res):
+        assert torch.equal(x, y) and bool(x.any())
+
+
 def test_far_positions_and_scale(dev):
     """Positions around 2^31: the fraction of the turn is what counts. Negative positions turn back."""
     say("rope far")
