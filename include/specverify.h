@@ -410,7 +410,7 @@ typedef struct {
  * (pages that nobody holds any more become free); table_in itself is left as it was.
  * table_in [rows_in, max_pages_per_req], lens_in [rows_in], parent [R], table_out
  * [R, max_pages_per_req], lens_out [R], ref [num_pages] int32. Inputs and outputs must not
- * overlap (checked for the tables).
+ * overlap (checked for the tables and the lengths).
  */
 sv_status sv_fork_pages(const sv_pages_desc* desc, int32_t rows_in, const int32_t* table_in,
                         const int32_t* lens_in, const int32_t* parent, int32_t* table_out, int32_t* lens_out,

@@ -263,6 +263,9 @@ sv_status sv_fork_pages(const sv_pages_desc* desc, int32_t rows_in, const int32_
     const uintptr_t in = (uintptr_t)table_in, out = (uintptr_t)table_out;
     if (in < out + 4ull * d.num_reqs * d.max_pages_per_req && out < in + 4ull * rows_in * d.max_pages_per_req)
         return fail(SV_ERR_INVALID_ARG, "sv_fork_pages: table_in and table_out overlap");
+    const uintptr_t li = (uintptr_t)lens_in, lo = (uintptr_t)lens_out;
+    if (li < lo + 4ull * d.num_reqs && lo < li + 4ull * rows_in)
+        return fail(SV_ERR_INVALID_ARG, "sv_fork_pages: lens_in and lens_out overlap");
     if (inject_launch_fault()) return fail(SV_ERR_HIP, "sv_fork_pages: injected launch failure");
     return launched(sv::launch_fork(d, rows_in, table_in, lens_in, parent, table_out, lens_out, ref,
                                     (hipStream_t)stream),

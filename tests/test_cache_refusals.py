@@ -98,6 +98,16 @@ def test_window_descriptor(lib, kw, window, sinks, status, msg):
     assert lib.sv_window_attn_workspace_size(ctypes.byref(d)) == 0
 
 
+@pytest.mark.parametrize("kw", [
+    dict(R=65535, block=1, total_q_max=1, Hq=2 ** 31 - 1, Hkv=2 ** 31 - 1, d=4, max_pages_per_req=1 << 16, page_size=64,
+         max_kv_len=1 << 22, kv_split=64, dtype=B.SV_F32),  # 2^32 lists for 2^31 blocks: just inside 64 bits
+    dict(R=1, block=16, total_q_max=1, Hq=1 << 22, Hkv=1, d=256, kv_split=64, dtype=B.SV_F32)])
+def test_window_calls_beyond_a_launch(lib, kw):
+    d = B.window_desc(B.attn_desc(**{**WINDOW, **kw}), 2 ** 31 - 1, 0)
+    assert lib.sv_window_attn(ctypes.byref(d), *[fake(i) for i in range(9)], BIG, None) == UNSUPPORTED
+    assert "one launch" in B.last_error(), B.last_error()
+
+
 def test_window_arguments(lib):
     d = B.window_desc(B.attn_desc(**{**WINDOW, "R": 2, "total_q_max": 2}), 6000, 4)
     need = B.window_attn_workspace_size(d)
@@ -158,6 +168,9 @@ def test_pages_arguments(lib):
     for off in (4 * 3 * 10, -4 * 8 * 10):
         p[3] = ctypes.c_void_p(p[0].value + off)
         assert lib.sv_fork_pages(r, 3, *p, None) == HIP, off
+    for off, status in ((0, INVALID), (4 * 2, INVALID), (-4 * 7, INVALID), (4 * 3, HIP), (-4 * 8, HIP)):  # the lengths
+        p[4] = ctypes.c_void_p(p[1].value + off)
+        assert lib.sv_fork_pages(r, 3, *p, None) == status, off
     p = [fake(i) for i in range(3)]
     assert lib.sv_release_pages(r, -1, 0, *p, None) == INVALID and lib.sv_release_pages(r, 1, -1, *p, None) == INVALID
     assert lib.sv_compact_pages(r, -1, *[fake(i) for i in range(5)], fake(9), BIG, None) == INVALID
