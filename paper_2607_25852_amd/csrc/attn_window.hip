@@ -936,8 +936,9 @@ hipError_t launch_window(const sv_window_desc& w, const WindowPlan& plan, const 
     a.maxp = d.max_pages_per_req;
     a.num_pages = d.num_pages;
     a.max_kv_len = d.max_kv_len;
-    a.window = w.window;
-    a.sinks = w.sinks;
+    // (no position is as far: differences with them stay inside 32 bits)
+    a.window = std::min(w.window, d.max_kv_len);
+    a.sinks = std::min(w.sinks, d.max_kv_len);
     a.splits = plan.splits;
     a.split_tiles = plan.split_tiles;
     a.nrb = plan.row_blocks;

@@ -124,6 +124,20 @@ def test_long_windows(dev, dtype):
         check(s)
 
 
+@pytest.mark.parametrize("Hq,d,page,k,ctx,window", [
+    (4, 64, 1, [5, 2], [2700, 1500], 2500), (4, 128, 1, [5, 2], [2700, 1500], 2500), (8, 128, 2, [16, 1], [3500, 2100], 3400),
+    (16, 64, 1, [16, 9], [2300, 1100], 2200), (16, 128, 1, [16, 9], [2300, 1100], 2200), (2, 64, 8, [3], [9500], 9000),
+    (2, 128, 16, [3], [17500], 17000)])
+def test_lists_longer_than_the_staged_pages(dev, Hq, d, page, k, ctx, window):
+    """One work item walks more page ids than are staged at a time; also with a page missing near the end."""
+    s = make(dev, 21, k, ctx, Hq, 1, d, page, "bf16", window, 70)
+    s["split"] = 1 << 20
+    say("window staged pages", Hq, d, page)
+    check(s)
+    s["table"][0, (ctx[0] - 100) // page] = -1
+    check(s)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_scores_of_every_size(dev, dtype):
     """Large and growing scores (the maximum moves), scores below -1e30, a given scale."""
