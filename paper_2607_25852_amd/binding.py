@@ -206,8 +206,8 @@ def _rows_ptr(t, stride: int, name: str) -> int:
     """Device pointer of rows [n, heads, d] that lie `stride` elements apart (0: dense)."""
     if isinstance(t, int):
         return t
-    n, heads, d = t.shape
-    want, st = stride or heads * d, t.stride()
+    (n, heads, d), st = t.shape, t.stride()
+    want = stride or heads * d
     if st != (want, d, 1) and ((n > 1 and st[0] != want) or (heads > 1 and st[1] != d) or (d > 1 and st[2] != 1)):
         raise ValueError(f"{name}: strides {st} are not those of rows {want} elements apart")
     return t.data_ptr()
@@ -224,9 +224,10 @@ def _stream(stream) -> Optional[int]:
 def _run(fn, desc, like, stream, *args):
     """fn(desc, *args, stream) on the device of tensor `like`: its current stream unless one is given."""
     import torch
-    dev = like.device.index if isinstance(like, torch.Tensor) else None
-    if dev is None or dev == torch.cuda.current_device():
-        _check(fn(ctypes.byref(desc), *args, _stream(stream)))
+    dev, cur = -1 if isinstance(like, int) else like.get_device(), torch.cuda.current_device()
+    if dev < 0 or dev == cur:
+        _check(fn(ctypes.byref(desc), *args,
+                  torch._C._cuda_getCurrentRawStream(cur) if stream is None else _stream(stream)))
         return
     with torch.cuda.device(dev):
         _check(fn(ctypes.byref(desc), *args, _stream(stream)))

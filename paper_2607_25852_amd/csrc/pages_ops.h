@@ -127,6 +127,7 @@ struct ReserveArgs {
     int32_t* upto;        // [R] demands of requests 0 .. i
     int32_t* copies;      // [R] copies of requests 0 .. i
     int32_t* chunk_free;  // [chunks] free pages of each chunk
+    const int32_t* was;   // [num_pages] ref, or a copy of it from before the call
 };
 
 // the last request whose first entry is at or before e (start[0] = 0, non-decreasing)
@@ -191,7 +192,7 @@ __device__ inline void reserve_demands(const ReserveArgs& a, ReserveLds<NT>& lds
         x.c = (a.ctx[x.i] >> a.log2P) + ((int)e - lds.start[x.i]);
         x.at = x.i * a.maxp + x.c;
         x.page = a.table[x.at];
-        x.holders = (unsigned)x.page < (unsigned)a.num_pages ? max(a.ref[x.page], 1) : 0;
+        x.holders = (unsigned)x.page < (unsigned)a.num_pages ? max(a.was[x.page], 1) : 0;
         return x;
     };
     // each thread's first entry is read once (a round's batch rarely has more)
@@ -311,7 +312,7 @@ __device__ inline uint32_t reserve_chunk(const ReserveArgs& a, int b, uint32_t b
         const int p0 = b * kPageChunk + k0 + 4 * tid;
         int r[4];
         uint32_t m = 0;
-        for (int x = 0; x < 4; x++) r[x] = p0 + x < a.num_pages && k0 + 4 * tid + x < kPageChunk ? a.ref[p0 + x] : 1;
+        for (int x = 0; x < 4; x++) r[x] = p0 + x < a.num_pages && k0 + 4 * tid + x < kPageChunk ? a.was[p0 + x] : 1;
         for (int x = 0; x < 4; x++) m += r[x] == 0;
         uint32_t total, rank = base + block_scan<NT>(m, wsum, total);
         for (int x = 0; x < 4; x++) {
@@ -348,7 +349,7 @@ __device__ inline void reserve_assign(const ReserveArgs& a, int b, uint32_t* wsu
 template <int NT>
 __device__ inline void reserve_alone(const ReserveArgs& a, ReserveLds<NT>& lds) {
     uint32_t n = 0, F;
-    for (int p = threadIdx.x; p < a.num_pages; p += NT) n += a.ref[p] == 0;
+    for (int p = threadIdx.x; p < a.num_pages; p += NT) n += a.was[p] == 0;
     reserve_demands<NT>(a, lds);
     block_scan<NT>(n, lds.wsum, F);
     __syncthreads();  // (the demands are in memory)

@@ -307,8 +307,9 @@ sv_status check_copy(const sv_copy_desc* desc) {
 ReservePlan plan_reserve(const sv_pages_desc& d) {
     ReservePlan p{};
     p.chunks = (d.num_pages + kPageChunkSize - 1) / kPageChunkSize;
-    // one workgroup for pages of one chunk (13.3 us for a round's reserve and release with 4000 pages; 14.2 us with a
-    // second kernel), a workgroup per chunk beyond (15.2 us with 24576 pages, one workgroup 20.4 us)
+    // one workgroup for pages of one chunk (11.8 us for a round's reserve and release with 4000 pages, 64 requests; 12.7 us
+    // with a second kernel), a workgroup per chunk beyond (13.3 us with 24576 pages; one workgroup, whose workspace
+    // does not fit the LDS there, 20.4 us)
     p.alone = p.chunks == 1;
     const size_t n = d.num_pages, R = d.num_reqs;
     p.writers = 0;

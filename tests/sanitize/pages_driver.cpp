@@ -105,9 +105,10 @@ Reserved reserve(const Pool& p, bool alone) {
         chunk_free(chunks);
     sv::ReserveArgs a{o.table.data(), o.ref.data(), p.ctx.data(), p.want.data(), o.src.data(), o.dst.data(),
                       o.tokens.data(), o.info.data(), p.R, p.maxp, p.pages, p.log2P, chunks, writers.data(),
-                      last.data(), demand.data(), copy_of.data(), upto.data(), copies.data(), chunk_free.data()};
+                      last.data(), demand.data(), copy_of.data(), upto.data(), copies.data(), chunk_free.data(), o.ref.data()};
     auto lds = std::make_unique<sv::ReserveLds<NT>>();
     if (alone) {
+        a.was = p.ref.data();
         hosthip::run_workgroup(NT, [&] { sv::reserve_alone<NT>(a, *lds); });
         return o;
     }
