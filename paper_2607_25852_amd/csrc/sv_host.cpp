@@ -345,14 +345,23 @@ WindowPlan plan_window(const sv_window_desc& w) {
     constexpr int T = kWindowTile;
     const long long tiles = longest_list(w.window, w.sinks, d.block, d.max_kv_len);
     const long long units = (long long)d.num_reqs * d.num_kv_heads * p.row_blocks;
-    // Lists are divided where the units alone leave compute units idle: into about 512 items (two workgroups per
-    // compute unit), of at least 4 tiles (fp32: 2). A divided list costs a second kernel (about 5 us). bf16,
-    // windows of 1024: 128 units of 128 rows take 30 us divided and 38 us whole, 256 units 43 and 37 us, 216
-    // units of 64-wide heads 28 and 22 us; items of 2 tiles take no less than of 4 (13.7 and 13.5 us for 32
-    // units of 8 rows). fp32, 64 units, windows of 128: items of 2 tiles 13 us, of 4 tiles 15 us.
-    long long per = tiles;
+    // Lists are divided where the units alone leave compute units idle, into items of at least 4 tiles (fp32: 2) that
+    // the GPU holds all at once: a few items more take a whole round longer (160 units of 128 rows, windows of 4000: 3
+    // splits 58 us, 4 splits 83 us). A divided list costs a second kernel (about 5 us).
+    // - bf16, 4 waves: two workgroups per compute unit, 512 items. Windows of 1024: 128 units of 128 rows take 30 us divided and
+    //   38 us whole, 256 units 43 and 37 us, 216 units of 64-wide heads 28 and 22 us; items of 2 tiles take no less
+    //   than of 4 (13.7 and 13.5 us for 32 units of 8 rows).
+    // - bf16, 8 waves: one workgroup per compute unit, 256 items (80 units of 256 rows, windows of 1000: 31 us, with 480 items
+    //   40 us; 160 units undivided 43 us, with 480 items 50 us). Twice as many even out what the rows differ, where items keep
+    //   32 tiles (160 units, windows of 8192: 184 us, undivided 240 us; 128 units, 32768: 482 us, with 256 items 520 us).
+    // - fp32: two workgroups per compute unit (160 units, windows of 2000: 3 splits 55 us, 4 splits 64 us). From 192 units
+    //   on long lists alone are worth it (256 units, windows of 512: 29 us whole and 30.5 us in halves, of 1024 51 and
+    //   47 us, of 2048 103 and 84 us). 64 units, windows of 128: items of 2 tiles 13 us, of 4 tiles 15 us.
+    long long per = tiles, most = 1;
+    if (p.waves == 8) most = tiles * units < 32 * 512 ? 256 / units : 512 / units;
+    else if (units < 192 || (d.dtype == SV_F32 && tiles >= 12)) most = 512 / units;
     if (d.kv_split > 0) per = std::max<long long>(1, d.kv_split / T);
-    else if (units < 192) per = std::max<long long>(d.dtype == SV_F32 ? 2 : 4, (tiles * units + 511) / 512);
+    else if (most > 1) per = std::max<long long>(d.dtype == SV_F32 ? 2 : 4, (tiles + most - 1) / most);
     p.split_tiles = (int)std::min(per, tiles);
     p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
     // All four waves on the same 32 rows, two tiles at a time: a step takes as long as one of two waves on one tile
