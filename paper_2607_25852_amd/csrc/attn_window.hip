@@ -216,10 +216,15 @@ __device__ __forceinline__ bool find_item(const WindowArgs& a, int block_rows, I
 // its products (fp32 products run at a sixteenth of the bf16 rate). With 32 rows per wave (twice the
 // products per load, half the waves) 8 requests of 5 positions and windows of 512 took 26.8 us, with 16
 // rows 20.3 us; with the next tile's keys loaded ahead 21.7 instead of 20.7 us, 32 requests 47 instead of 43 us.
+// So what hides the latency is workgroups: the rows stay in LDS, which leaves room for three of them (147 registers) where
+// rows in registers left two (45 requests 57 us, then 77 us). Four (128 registers) spill: 24 instead of 21 us.
 template <int DG>
-__global__ __launch_bounds__(256, DG == 4 ? 1 : 2) void window_f32_kernel(WindowArgs a) {
+__global__ __launch_bounds__(256, DG == 4 ? 2 : 3) void window_f32_kernel(WindowArgs a) {
     constexpr int NW = 4, NB = 4 * DG;  // waves; 16-dim blocks of the scores' sum
-    __shared__ float s_o[NW][DG * 4][4][64];
+    __shared__ union {
+        f32x4 q[NB][64];  // the rows, as every wave's lanes take them
+        float o[NW][DG * 4][4][64];
+    } u;
     __shared__ float s_ml[NW][2][64];
     Item x;
     if (!find_item(a, 16, x)) return;
@@ -237,12 +242,12 @@ __global__ __launch_bounds__(256, DG == 4 ? 1 : 2) void window_f32_kernel(Window
     const bool row_ok = n < x.M;
     const int rr = x.row0 + (row_ok ? n : 0), jq = rr / a.G, p = x.L + jq;  // row of the kv-head group, its position
     const size_t orow = (size_t)(x.q0 + jq) * a.Hq + x.h * a.G + rr % a.G;
-    f32x4 qf[NB];
 #pragma unroll
-    for (int b = 0; b < NB; b++) {
+    for (int b = w; b < NB; b += NW) {
         const int d = 16 * b + 4 * q;
-        qf[b] = row_ok && d < HD ? *(const f32x4*)((const float*)a.q + orow * HD + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+        u.q[b][lane] = row_ok && d < HD ? *(const f32x4*)((const float*)a.q + orow * HD + d) : f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    __syncthreads();
     f32x4 o[DG * 4];
 #pragma unroll
     for (int d = 0; d < DG * 4; d++) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -276,12 +281,14 @@ __global__ __launch_bounds__(256, DG == 4 ? 1 : 2) void window_f32_kernel(Window
         if (!any) continue;
         f32x4 s = {0.f, 0.f, 0.f, 0.f}, s2 = s;  // two chains
 #pragma unroll
-        for (int b = 0; b < NB; b++)
+        for (int b = 0; b < NB; b++) {
+            const f32x4 qf = u.q[b][lane];
 #pragma unroll
             for (int c = 0; c < 4; c += 2) {
-                s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][c], qf[b][c], s, 0, 0, 0);
-                s2 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][c + 1], qf[b][c + 1], s2, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][c], qf[c], s, 0, 0, 0);
+                s2 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][c + 1], qf[c + 1], s2, 0, 0, 0);
             }
+        }
         // keys s0 + 4 q + e of row n
         float mx = -INFINITY;
 #pragma unroll
@@ -316,10 +323,11 @@ __global__ __launch_bounds__(256, DG == 4 ? 1 : 2) void window_f32_kernel(Window
     l += __shfl_xor(l, 32, 64);
     s_ml[w][0][lane] = m;
     s_ml[w][1][lane] = l;
+    __syncthreads();  // (the rows are no longer read)
 #pragma unroll
     for (int d = 0; d < DG * 4; d++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) s_o[w][d][e][lane] = o[d][e];
+        for (int e = 0; e < 4; e++) u.o[w][d][e][lane] = o[d][e];
     __syncthreads();
     float M = -INFINITY, lt = 0.0f, wt[NW];
 #pragma unroll
@@ -341,7 +349,7 @@ __global__ __launch_bounds__(256, DG == 4 ? 1 : 2) void window_f32_kernel(Window
 #pragma unroll
         for (int c = 0; c < 4; c++)
 #pragma unroll
-            for (int z = 0; z < NW; z++) v[c] += s_o[z][y / 4 * 4 + c][y % 4][lane] * wt[z];
+            for (int z = 0; z < NW; z++) v[c] += u.o[z][y / 4 * 4 + c][y % 4][lane] * wt[z];
         const int d = 64 * (y / 4) + 16 * q + 4 * (y % 4);
         if (row_ok && d < HD) {
             *(f32x4*)(out + d) = v * inv;
