@@ -350,7 +350,8 @@ WindowPlan plan_window(const sv_window_desc& w) {
     // splits 58 us, 4 splits 83 us). A divided list costs a second kernel (about 5 us).
     // - bf16, 4 waves: two workgroups per compute unit, 512 items. Windows of 1024: 128 units of 128 rows take 30 us divided and
     //   38 us whole, 256 units 43 and 37 us, 216 units of 64-wide heads 28 and 22 us; items of 2 tiles take no less
-    //   than of 4 (13.7 and 13.5 us for 32 units of 8 rows).
+    //   than of 4 (13.7 and 13.5 us for 32 units of 8 rows). Long lists in halves up to 256 units (256 units of 128 rows: windows
+    //   of 2000 57 us either way, of 4000 84 us, whole 96 us; 216 units, 4000, most contexts short: 54 and 83 us).
     // - bf16, 8 waves: one workgroup per compute unit, 256 items (80 units of 256 rows, windows of 1000: 31 us, with 480 items
     //   40 us; 160 units undivided 43 us, with 480 items 50 us). Twice as many even out what the rows differ, where items keep
     //   32 tiles (160 units, windows of 8192: 184 us, undivided 240 us; 128 units, 32768: 482 us, with 256 items 520 us).
@@ -361,7 +362,7 @@ WindowPlan plan_window(const sv_window_desc& w) {
     long long per = tiles, most = 1;
     if (p.waves == 8) most = tiles * units < 32 * 512 ? 256 / units : 512 / units;
     else if (d.dtype == SV_F32 && tiles >= 8) most = (d.head_dim <= 64 ? 1024 : d.head_dim <= 128 ? 768 : 512) / units;
-    else if (units < 192) most = 512 / units;
+    else if (units < 192 || (d.dtype == SV_BF16 && tiles >= 32)) most = 512 / units;
     if (d.kv_split > 0) per = std::max<long long>(1, d.kv_split / T);
     else if (most > 1) per = std::max<long long>(d.dtype == SV_F32 ? 2 : 4, (tiles + most - 1) / most);
     p.split_tiles = (int)std::min(per, tiles);
