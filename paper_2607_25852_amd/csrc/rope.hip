@@ -30,7 +30,8 @@ struct RopeArgs {
     int R, total, Hq, Hkv, d, pairs, axes, cycle, log2P, maxp, num_pages;
     int section[SV_MAX_ROPE_AXES];
     float scale;
-    int tasks, tasks_per_head, turns_per_head;  // of a row; of a head of q or k; those that turn pairs
+    int tasks, tasks_per_head;        // of a row; of a head of q or k
+    int turn_chunks, turns, copy_chunks;  // dims of either half: chunks of pairs, with single pairs; chunks passed through
 };
 
 constexpr int kMaxPairs = 512;
@@ -48,9 +49,10 @@ __device__ inline int pair_axis(const RopeArgs& a, int p) {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-template <typename T> struct Chunk;  // 16 bytes of a row as floats
+template <typename T> struct Chunk;  // 16 bytes of a row as floats, at any element
 template <> struct Chunk<float> {
     static constexpr int N = 4;
+    typedef u32x4 Any __attribute__((aligned(4)));
     static __device__ void get(const u32x4& x, float* f) {
         f[0] = __uint_as_float(x.x), f[1] = __uint_as_float(x.y), f[2] = __uint_as_float(x.z),
         f[3] = __uint_as_float(x.w);
@@ -61,6 +63,7 @@ template <> struct Chunk<float> {
 };
 template <> struct Chunk<uint16_t> {
     static constexpr int N = 8;
+    typedef u32x4 Any __attribute__((aligned(2)));
     static __device__ void get(const u32x4& x, float* f) {
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
@@ -82,16 +85,18 @@ __device__ inline float load1(const uint16_t* p) { return __uint_as_float((uint3
 __device__ inline void store1(float* p, float f) { *p = f; }
 __device__ inline void store1(uint16_t* p, float f) { *p = f2bf(f); }
 
-// grid (row, part of the row's tasks). VEC: a task turns the pairs of one chunk (adjacent dims) or of
-// two chunks (dims of either half), or copies a chunk; else it turns one pair, or copies one element. STREAM: rows
-// are read and written past the caches. (Two tasks per thread in flight, the first ones under the row's angles and
+// grid (row, part of the row's tasks). A task turns the pairs of one chunk (adjacent dims) or of two chunks (dims of
+// either half), or copies a chunk. Halves that are no whole chunks have their second chunks at any element, and single pairs
+// and elements at the end (512 rows of 80 heads with 30 pairs 8.3 us, with 32 pairs 6.6 us; a task per pair and
+// element 19 us). STREAM: rows are read and written past the caches. (Two tasks per thread in flight, the first ones under the row's angles and
 // page, took 3.5 us instead of 3.2 for 4 rows and 53 instead of 48 for 14996.)
-template <typename T, bool ADJ, bool VEC, bool STREAM>
+template <typename T, bool ADJ, bool STREAM>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     __shared__ float2 cs[kMaxPairs];
     __shared__ long long s_slot;  // the row's slot in the cache's first kv-head, -1: none
     __shared__ int s_ok;
-    constexpr int N = VEC ? Chunk<T>::N : 1;
+    constexpr int N = Chunk<T>::N;
+    typedef typename Chunk<T>::Any Any;
     const int row = blockIdx.x, tid = threadIdx.x;
     if (row >= a.qo[a.R]) return;
     if (tid < 64) {
@@ -132,19 +137,33 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
     if (!s_ok) return;
     const long long slot = s_slot;
     const int heads = a.Hq + a.Hkv, d = a.d, half = a.pairs;
-    auto chunk = [](const T* p) {
-        if constexpr (STREAM) return __builtin_nontemporal_load((const u32x4*)p);
-        else return *(const u32x4*)p;
+    auto chunk = [](const T* p) -> u32x4 {
+        if constexpr (STREAM) return __builtin_nontemporal_load((const Any*)p);
+        else return *(const Any*)p;
     };
     auto store = [](T* p, u32x4 x) {
-        if constexpr (STREAM) __builtin_nontemporal_store(x, (u32x4*)p);
-        else *(u32x4*)p = x;
+        if constexpr (STREAM) __builtin_nontemporal_store((Any)x, (Any*)p);
+        else *(Any*)p = x;
     };
     for (int t = blockIdx.y * 256 + tid; t < a.tasks; t += gridDim.y * 256) {
         const bool value = t >= heads * a.tasks_per_head;
-        const int per = value ? d / N : a.tasks_per_head;
-        const int u = value ? t - heads * a.tasks_per_head : t;
-        const int hx = u / per, c = u % per;  // head, task in the head
+        // head and task in the head; the kinds of tasks one after the other, so that a wave has one kind (with the kinds of
+        // each head together 10.5 instead of 8.3 us for 30 pairs)
+        int u = value ? t - heads * a.tasks_per_head : t, per = value ? d / N : a.tasks_per_head, c0 = 0;
+        if (!ADJ && !value) {
+            const int ends[4] = {a.turn_chunks, a.turns, a.turns + a.copy_chunks, a.tasks_per_head};
+            per = ends[0];
+#pragma unroll
+            for (int x = 0; x < 3; x++)
+                if (u >= heads * per) {
+                    u -= heads * per;
+                    c0 = ends[x];
+                    per = ends[x + 1] - c0;
+                } else {
+                    break;
+                }
+        }
+        const int hx = u / per, c = c0 + u % per;
         const bool key = !value && hx >= a.Hq;
         if ((value || key) && slot < 0) continue;
         const int h = key ? hx - a.Hq : hx;
@@ -152,29 +171,25 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
                                                                         : a.q + row * a.q_stride)) + (size_t)h * d;
         T* dst = value || key ? (T*)(value ? a.vc : a.kc) + ((size_t)slot + ((size_t)h << a.log2P)) * d
                               : (T*)a.q_out + ((size_t)row * a.Hq + h) * d;
-        if (value || c >= a.turns_per_head) {
-            const int at = value ? c * N : 2 * half + (c - a.turns_per_head) * N;
-            if constexpr (VEC) store(dst + at, chunk(src + at));
-            else dst[at] = src[at];
-            continue;
-        }
-        if constexpr (!VEC) {
-            const int i = ADJ ? 2 * c : c, j = ADJ ? 2 * c + 1 : c + half;
-            const float x = load1(src + i), y = load1(src + j);
-            const float2 w = cs[c];
-            store1(dst + i, x * w.x - y * w.y);
-            store1(dst + j, y * w.x + x * w.y);
+        if (value) {
+            store(dst + c * N, chunk(src + c * N));
         } else if constexpr (ADJ) {
-            float x[N];
-            Chunk<T>::get(chunk(src + c * N), x);
+            u32x4 raw = chunk(src + c * N);
+            if (c * N < 2 * half) {
+                float x[N];
+                Chunk<T>::get(raw, x);
 #pragma unroll
-            for (int e = 0; e < N; e += 2) {
-                const float2 w = cs[(c * N + e) / 2];
-                const float u0 = x[e] * w.x - x[e + 1] * w.y, u1 = x[e + 1] * w.x + x[e] * w.y;
-                x[e] = u0, x[e + 1] = u1;
+                for (int e = 0; e < N; e += 2) {
+                    const int p = (c * N + e) / 2;
+                    if (p >= half) continue;
+                    const float2 w = cs[p];
+                    const float u0 = x[e] * w.x - x[e + 1] * w.y, u1 = x[e + 1] * w.x + x[e] * w.y;
+                    x[e] = u0, x[e + 1] = u1;
+                }
+                raw = Chunk<T>::put(x);
             }
-            store(dst + c * N, Chunk<T>::put(x));
-        } else {
+            store(dst + c * N, raw);
+        } else if (c < a.turn_chunks) {
             float x[N], y[N];
             Chunk<T>::get(chunk(src + c * N), x);
             Chunk<T>::get(chunk(src + half + c * N), y);
@@ -186,6 +201,18 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
             }
             store(dst + c * N, Chunk<T>::put(x));
             store(dst + half + c * N, Chunk<T>::put(y));
+        } else if (c < a.turns) {
+            const int p = a.turn_chunks * N + (c - a.turn_chunks);
+            const float x = load1(src + p), y = load1(src + half + p);
+            const float2 w = cs[p];
+            store1(dst + p, x * w.x - y * w.y);
+            store1(dst + half + p, y * w.x + x * w.y);
+        } else if (c < a.turns + a.copy_chunks) {
+            const int at = 2 * half + (c - a.turns) * N;
+            store(dst + at, chunk(src + at));
+        } else {
+            const int at = 2 * half + a.copy_chunks * N + (c - a.turns - a.copy_chunks);
+            dst[at] = src[at];
         }
     }
 }
@@ -232,31 +259,29 @@ hipError_t launch_rope(const sv_rope_desc& d, const void* q, const void* k_new, 
     a.num_pages = d.num_pages;
     a.scale = d.scale == 0.0f ? 1.0f : d.scale;
     const bool adj = d.pairing == SV_ROPE_ADJACENT;
-    // chunks hold whole pairs (adjacent dims), or the same pairs of either half
-    const bool vec = (adj ? d.rot_dim : d.rot_dim / 2) % N == 0;
-    const int n = vec ? N : 1;
-    a.turns_per_head = vec && adj ? d.rot_dim / N : a.pairs / n;
-    a.tasks_per_head = a.turns_per_head + (d.head_dim - d.rot_dim) / n;
-    a.tasks = (d.num_q_heads + d.num_kv_heads) * a.tasks_per_head + d.num_kv_heads * (d.head_dim / n);
+    const int rest = d.head_dim - d.rot_dim;
+    a.turn_chunks = a.pairs / N;
+    a.turns = a.turn_chunks + a.pairs % N;
+    a.copy_chunks = rest / N;
+    a.tasks_per_head = adj ? d.head_dim / N : a.turns + a.copy_chunks + rest % N;
+    a.tasks = (d.num_q_heads + d.num_kv_heads) * a.tasks_per_head + d.num_kv_heads * (d.head_dim / N);
     // a row is divided among workgroups where the rows alone are too few
     const int parts = std::max(1, std::min((a.tasks + 255) / 256, 2048 / d.total_max));
     const dim3 grid(d.total_max, parts);
     // Rows of many megabytes go past the caches both ways. 14996 rows (138 MB in, as much out): 47 us, through the caches
     // 55 us from memory and 47 us where the rows still lie in the last-level cache; 7500 rows 26 us, 32 and 23 us. Fewer rows
-    // were just written and are about to be read: 512 rows 6.5 us past the caches, 5.9 us through them.
-    const bool past = (size_t)d.total_max * (d.num_q_heads + 2 * d.num_kv_heads) * d.head_dim * esz > (size_t)64 << 20;
-#define SV_ROPE(T, ADJ, VEC, S) hipLaunchKernelGGL((rope_kernel<T, ADJ, VEC, S>), grid, dim3(256), 0, stream, a)
-#define SV_ROPE_VEC(T, ADJ) \
-    if (!vec) SV_ROPE(T, ADJ, false, false); \
-    else if (past) SV_ROPE(T, ADJ, true, true); \
-    else SV_ROPE(T, ADJ, true, false)
+    // were just written and are about to be read: 512 rows 6.5 us past the caches, 5.9 us through them. Halves that are no
+    // whole chunks write lines in parts, which the caches put together (14996 rows with 55 pairs 79 us, past them 121 us).
+    const bool past = (adj || a.pairs % N == 0) && (size_t)d.total_max * (d.num_q_heads + 2 * d.num_kv_heads) * d.head_dim * esz > (size_t)64 << 20;
+#define SV_ROPE(T, ADJ) \
+    if (past) hipLaunchKernelGGL((rope_kernel<T, ADJ, true>), grid, dim3(256), 0, stream, a); \
+    else hipLaunchKernelGGL((rope_kernel<T, ADJ, false>), grid, dim3(256), 0, stream, a)
 #define SV_ROPE_TYPE(T) \
-    if (adj) { SV_ROPE_VEC(T, true); } \
-    else { SV_ROPE_VEC(T, false); }
+    if (adj) { SV_ROPE(T, true); } \
+    else { SV_ROPE(T, false); }
     if (d.dtype == SV_F32) { SV_ROPE_TYPE(float) }
     else { SV_ROPE_TYPE(uint16_t) }
 #undef SV_ROPE_TYPE
-#undef SV_ROPE_VEC
 #undef SV_ROPE
     return hipGetLastError();
 }

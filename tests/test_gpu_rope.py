@@ -107,6 +107,17 @@ def test_parts_of_a_head(dev, d, sections, pairing, dtype):
     check(make(dev, 2, [3, 1, 2], [9, 0, 100], 6, 3, d, 8, dtype, sections, "blocks", pairing, pad=8))
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 24), ("f32", 12)])
+@pytest.mark.parametrize("pairing", ["halves", "adjacent"])
+def test_every_count_of_pairs(dev, dtype, d, pairing):
+    """Halves of whole 16-byte chunks, of parts of them, and both; what passes through likewise; in place too."""
+    for pairs in range(1, d // 2 + 1):
+        say("rope pairs", dtype, pairing, pairs)
+        check(make(dev, 30 + pairs, [3, 1, 6], [9, 0, 30], 3, 2, d, 8, dtype, (pairs,), "blocks", pairing))
+        s = make(dev, 60 + pairs, [2, 5], [0, 17], 5, 1, d, 16, dtype, (pairs,), "blocks", pairing, fused=False)
+        check(s, q_out=s["q"])
+
+
 @pytest.mark.parametrize("page", [1, 2, 64, 4096])
 def test_pages(dev, page):
     say("rope page", page)
