@@ -354,13 +354,14 @@ WindowPlan plan_window(const sv_window_desc& w) {
     //   of 2000 57 us either way, of 4000 84 us, whole 96 us; 216 units, 4000, most contexts short: 54 and 83 us).
     // - bf16, 8 waves: one workgroup per compute unit, 256 items (80 units of 256 rows, windows of 1000: 31 us, with 480 items
     //   40 us; 160 units undivided 43 us, with 480 items 50 us). Twice as many even out what the rows differ, where items keep
-    //   32 tiles (160 units, windows of 8192: 184 us, undivided 240 us; 128 units, 32768: 482 us, with 256 items 520 us).
+    //   20 tiles (160 units, windows of 8192: 184 us, undivided 240 us; 128 units, 32768: 482 us, with 256 items 520 us; 136
+    //   units, 5000: 113 and 153 us, 200 units, 3500: 121 and 115 us, 240 units, 2400: 100 and 87 us).
     // - fp32: three workgroups per compute unit, four of 64-wide heads and two of heads above 128. Lists of less than 8 tiles
     //   where there are few units alone. 256 units of 16 rows, windows of 512: 27 us in 3 splits, 30 us whole; of
     //   230 (6 tiles) 20 us in 3 splits, 19 us whole; 160 units of 64-wide heads, 2000: 6 splits 31 us, 4 splits 35 us; 64
     //   units, windows of 128: items of 2 tiles 13 us, of 4 tiles 15 us.
     long long per = tiles, most = 1;
-    if (p.waves == 8) most = tiles * units < 32 * 512 ? 256 / units : 512 / units;
+    if (p.waves == 8) most = tiles * units < 20 * 512 ? 256 / units : 512 / units;
     else if (d.dtype == SV_F32 && tiles >= 8) most = (d.head_dim <= 64 ? 1024 : d.head_dim <= 128 ? 768 : 512) / units;
     else if (units < 192 || (d.dtype == SV_BF16 && tiles >= 32)) most = 512 / units;
     if (d.kv_split > 0) per = std::max<long long>(1, d.kv_split / T);
