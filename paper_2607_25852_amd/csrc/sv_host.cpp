@@ -374,8 +374,12 @@ WindowPlan plan_window(const sv_window_desc& w) {
     // units 55 and 48 us) and walks its whole list (32 units in 5 splits 14.2 and 13.8 us).
     p.few = d.dtype == SV_BF16 && rows <= 32 && (d.head_dim == 64 || (units <= 256 && p.splits == 1));
     // Where the rows may differ, every XCD gets two (request, split)s at least and there is enough to do that the
-    // order repays finding it (0.5 to 1 us: 3900 tiles in all lose 1 of 22 us, 9700 win 1 of 56)
-    p.by_rows = d.block > 1 && d.num_reqs <= 64 && (long long)d.num_reqs * p.splits >= 16 && tiles * units >= 8192;
+    // order repays finding it (0.5 to 1 us). Tiles in all: 128-row blocks of four waves, of which two share a compute unit,
+    // from 4096 on (3900 tiles lose 1 of 22 us, 5200 win 4 of 43, 6100 win 4 of 45); others from 8192 (four waves on 32 rows, 6400
+    // lose 1 of 25 us; eight waves, 6200 lose 2 of 60; fp32, 3600 lose 2 of 55).
+    const bool pairs = d.dtype == SV_BF16 && p.waves == 4 && !p.few;
+    p.by_rows = d.block > 1 && d.num_reqs <= 64 && (long long)d.num_reqs * p.splits >= 16 &&
+                tiles * units >= (pairs ? 4096 : 8192);
     if (p.splits > 1) {
         const size_t n = (size_t)p.splits * d.total_q_max * d.num_q_heads;
         p.part_o_bytes = n * d.head_dim * sizeof(float);
