@@ -48,7 +48,7 @@ def check_reserve(torch, table, refs, ctx, new, page):
 
 
 SHAPES = [(1, 1, 1, 1), (3, 4, 16, 20), (17, 9, 64, 150), (64, 12, 16, 700), (200, 5, 1, 2000), (1100, 3, 8, 4096),
-          (9, 40, 4, 4097), (4096, 2, 64, 9000), (50, 6, 16, 70001)]
+          (4096, 2, 4, 4096), (9, 40, 4, 4097), (4096, 2, 64, 9000), (50, 6, 16, 70001)]
 
 
 @pytest.mark.parametrize("R,cols,page,pages", SHAPES)
