@@ -205,7 +205,7 @@ __device__ __forceinline__ bool find_item(const WindowArgs& a, int block_rows, I
 // ---------------------------------------------------------------------------------
 // fp32 MFMA kernel
 // ---------------------------------------------------------------------------------
-// A workgroup of four waves takes one item of up to 16 query rows; wave w has keys 16 w .. + 15 of every tile.
+// A workgroup of four waves takes one item of RG groups of 16 query rows; wave w has keys 16 w .. + 15 of every tile.
 // v_mfma_f32_16x16x4_f32 multiplies and adds in fp32. Its k index is free as long as both operands agree, which
 // lets every lane load 16 bytes at a time straight into the operands (lane = 16 q + n):
 //   scores S^T = K Q^T: step (b, c) takes dim 16 b + 4 q + c of key n and of row n;
@@ -213,21 +213,21 @@ __device__ __forceinline__ bool find_item(const WindowArgs& a, int block_rows, I
 //   O^T = V^T P^T: step e takes key 4 q + e, so P^T is where the scores were left; tile (g, c) of the
 //   output has dims 64 g + 4 n + c, and lane 16 q + n gets dims 64 g + 16 q + 4 e + c of row n.
 // Keys that no row sees are not loaded. Bound by the latency of a tile's loads (page, K and V) and by the chain of
-// its products (fp32 products run at a sixteenth of the bf16 rate). With 32 rows per wave (twice the
-// products per load, half the waves) 8 requests of 5 positions and windows of 512 took 26.8 us, with 16
-// rows 20.3 us; with the next tile's keys loaded ahead 21.7 instead of 20.7 us, 32 requests 47 instead of 43 us.
+// its products (fp32 products run at a sixteenth of the bf16 rate). With two groups of rows (twice the
+// products per load, half the waves) 8 requests of 5 positions and windows of 512 take 22.5 us, with one
+// 19.8 us; they pay where one would take more rounds of workgroups (plan_window). With the next tile's keys loaded ahead 21.7 instead of 20.7 us, 32 requests 47 instead of 43 us.
 // So what hides the latency is workgroups: the rows stay in LDS, which leaves room for three of them (147 registers) where
 // rows in registers left two (45 requests 57 us, then 77 us). Four (128 registers) spill: 24 instead of 21 us.
-template <int DG>
-__global__ __launch_bounds__(256, DG == 4 ? 2 : 3) void window_f32_kernel(WindowArgs a) {
+template <int DG, int RG>
+__global__ __launch_bounds__(256, DG * RG >= 4 ? 2 : 3) void window_f32_kernel(WindowArgs a) {
     constexpr int NW = 4, NB = 4 * DG;  // waves; 16-dim blocks of the scores' sum
     __shared__ union {
-        f32x4 q[NB][64];  // the rows, as every wave's lanes take them
+        f32x4 q[RG][NB][64];  // the rows, as every wave's lanes take them
         float o[NW][DG * 4][4][64];
     } u;
     __shared__ float s_ml[NW][2][64];
     Item x;
-    if (!find_item(a, 16, x)) return;
+    if (!find_item(a, 16 * RG, x)) return;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n = lane & 15, q = lane >> 4, HD = a.HD;
     const int32_t* __restrict__ pt = a.page_table + (size_t)x.i * a.maxp;
@@ -239,19 +239,29 @@ __global__ __launch_bounds__(256, DG == 4 ? 2 : 3) void window_f32_kernel(Window
         return pg < a.num_pages ? pg : -1;
     };
     int pg = page_of(x.t0);
-    const bool row_ok = n < x.M;
-    const int rr = x.row0 + (row_ok ? n : 0), jq = rr / a.G, p = x.L + jq;  // row of the kv-head group, its position
-    const size_t orow = (size_t)(x.q0 + jq) * a.Hq + x.h * a.G + rr % a.G;
+    // row n of group g: its place in the kv-head group
+    auto row_of = [&](int g) { return x.row0 + (16 * g + n < x.M ? 16 * g + n : 0); };
+    auto out_row = [&](int g) { return (size_t)(x.q0 + row_of(g) / a.G) * a.Hq + x.h * a.G + row_of(g) % a.G; };
+    int p[RG];  // the rows' positions
 #pragma unroll
-    for (int b = w; b < NB; b += NW) {
-        const int d = 16 * b + 4 * q;
-        u.q[b][lane] = row_ok && d < HD ? *(const f32x4*)((const float*)a.q + orow * HD + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int g = 0; g < RG; g++) {
+        p[g] = x.L + row_of(g) / a.G;
+        const float* src = (const float*)a.q + out_row(g) * HD;
+#pragma unroll
+        for (int b = w; b < NB; b += NW) {
+            const int d = 16 * b + 4 * q;
+            u.q[g][b][lane] = 16 * g + n < x.M && d < HD ? *(const f32x4*)(src + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
     }
     __syncthreads();
-    f32x4 o[DG * 4];
+    f32x4 o[RG][DG * 4];
+    float m[RG], l[RG];
 #pragma unroll
-    for (int d = 0; d < DG * 4; d++) o[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.0f;
+    for (int g = 0; g < RG; g++) {
+#pragma unroll
+        for (int d = 0; d < DG * 4; d++) o[g][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+        m[g] = -INFINITY, l[g] = 0.0f;
+    }
     for (int t = x.t0; t < x.t1; t++) {
         const int s0 = list_tile(x.list, t) * kTile + 16 * w;
         const int next = t + 1 < x.t1 ? page_of(t + 1) : -1;
@@ -271,96 +281,106 @@ __global__ __launch_bounds__(256, DG == 4 ? 2 : 3) void window_f32_kernel(Window
             vpg[e] = __shfl(pg, 4 * q + e, 64);
             const float* vp = (const float*)a.vc + row_at(max(vpg[e], 0), 4 * q + e);
 #pragma unroll
-            for (int g = 0; g < DG; g++) {
-                const int d = 64 * g + 4 * n;
-                vf[e][g] = vpg[e] >= 0 && d < HD ? *(const f32x4*)(vp + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int c = 0; c < DG; c++) {
+                const int d = 64 * c + 4 * n;
+                vf[e][c] = vpg[e] >= 0 && d < HD ? *(const f32x4*)(vp + d) : f32x4{0.f, 0.f, 0.f, 0.f};
             }
         }
         const bool any = __any(pg >= 0);
         pg = next;
         if (!any) continue;
-        f32x4 s = {0.f, 0.f, 0.f, 0.f}, s2 = s;  // two chains
 #pragma unroll
-        for (int b = 0; b < NB; b++) {
-            const f32x4 qf = u.q[b][lane];
+        for (int g = 0; g < RG; g++) {
+            if (g > 0 && x.M <= 16 * g) break;
+            f32x4 s = {0.f, 0.f, 0.f, 0.f}, s2 = s;  // two chains
 #pragma unroll
-            for (int c = 0; c < 4; c += 2) {
-                s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][c], qf[c], s, 0, 0, 0);
-                s2 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][c + 1], qf[c + 1], s2, 0, 0, 0);
+            for (int b = 0; b < NB; b++) {
+                const f32x4 qf = u.q[g][b][lane];
+#pragma unroll
+                for (int c = 0; c < 4; c += 2) {
+                    s = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][c], qf[c], s, 0, 0, 0);
+                    s2 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[b][c + 1], qf[c + 1], s2, 0, 0, 0);
+                }
             }
+            // keys s0 + 4 q + e of row n
+            float mx = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const int key = s0 + 4 * q + e;
+                const bool ok = (vpg[e] >= 0) & (key <= p[g]) & ((key < a.sinks) | (key > p[g] - a.window));
+                s[e] = ok ? (s[e] + s2[e]) * a.scale_log2 : -INFINITY;
+                mx = fmaxf(mx, s[e]);
+            }
+            mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float m_new = fmaxf(m[g], mx), ref = m_new == -INFINITY ? 0.0f : m_new;
+            const float alpha = m[g] == -INFINITY ? (l[g] != 0.0f ? 1.0f : 0.0f) : exp2f(m[g] - m_new);
+            m[g] = m_new;
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                s[e] = exp2f(s[e] - ref);
+                sum += s[e];
+            }
+            l[g] = l[g] * alpha + sum;
+#pragma unroll
+            for (int d = 0; d < DG * 4; d++) o[g][d] *= alpha;
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+#pragma unroll
+                for (int d = 0; d < DG * 4; d++)
+                    o[g][d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e][d / 4][d % 4], s[e], o[g][d], 0, 0, 0);
         }
-        // keys s0 + 4 q + e of row n
-        float mx = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const int key = s0 + 4 * q + e;
-            const bool ok = (vpg[e] >= 0) & (key <= p) & ((key < a.sinks) | (key > p - a.window));
-            s[e] = ok ? (s[e] + s2[e]) * a.scale_log2 : -INFINITY;
-            mx = fmaxf(mx, s[e]);
-        }
-        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-        const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.0f : m_new;
-        const float alpha = m == -INFINITY ? (l != 0.0f ? 1.0f : 0.0f) : exp2f(m - m_new);
-        m = m_new;
-        float sum = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            s[e] = exp2f(s[e] - ref);
-            sum += s[e];
-        }
-        l = l * alpha + sum;
-#pragma unroll
-        for (int d = 0; d < DG * 4; d++) o[d] *= alpha;
-#pragma unroll
-        for (int e = 0; e < 4; e++)
-#pragma unroll
-            for (int d = 0; d < DG * 4; d++)
-                o[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[e][d / 4][d % 4], s[e], o[d], 0, 0, 0);
     }
     // merge the waves' states; wave w finishes every fourth block of 16 dims
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    s_ml[w][0][lane] = m;
-    s_ml[w][1][lane] = l;
-    __syncthreads();  // (the rows are no longer read)
-#pragma unroll
-    for (int d = 0; d < DG * 4; d++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) u.o[w][d][e][lane] = o[d][e];
-    __syncthreads();
-    float M = -INFINITY, lt = 0.0f, wt[NW];
-#pragma unroll
-    for (int y = 0; y < NW; y++) M = fmaxf(M, s_ml[y][0][lane]);
-#pragma unroll
-    for (int y = 0; y < NW; y++) {
-        const float my = s_ml[y][0][lane], ly = s_ml[y][1][lane];
-        // (a part whose scores are all NaN has no maximum, but its sum counts)
-        wt[y] = my == -INFINITY ? (ly != 0.0f ? 1.0f : 0.0f) : exp2f(my - M);
-        lt += ly * wt[y];
-    }
-    const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
     const bool whole = a.splits == 1 || x.t1 - x.t0 == x.list.nt;
-    const size_t prow = (size_t)x.sp * a.total_q * a.Hq + orow;
-    float* out = whole ? (float*)a.out + orow * HD : a.part_o + prow * HD;
     float odd = 0.0f;  // NaN where a result is not finite
-    for (int y = w; y < DG * 4; y += NW) {  // dims 64 (y / 4) + 16 q + 4 (y % 4) + c
-        f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int c = 0; c < 4; c++)
+    for (int g = 0; g < RG; g++) {
+        if (g > 0 && x.M <= 16 * g) break;
+        const bool row_ok = 16 * g + n < x.M;
+        const size_t orow = out_row(g);
+        l[g] += __shfl_xor(l[g], 16, 64);
+        l[g] += __shfl_xor(l[g], 32, 64);
+        __syncthreads();  // (the rows, or the states of the group before, are no longer read)
+        s_ml[w][0][lane] = m[g];
+        s_ml[w][1][lane] = l[g];
 #pragma unroll
-            for (int z = 0; z < NW; z++) v[c] += u.o[z][y / 4 * 4 + c][y % 4][lane] * wt[z];
-        const int d = 64 * (y / 4) + 16 * q + 4 * (y % 4);
-        if (row_ok && d < HD) {
-            *(f32x4*)(out + d) = v * inv;
+        for (int d = 0; d < DG * 4; d++)
 #pragma unroll
-            for (int c = 0; c < 4; c++) odd = __builtin_fmaf(v[c], 0.0f, odd);
+            for (int e = 0; e < 4; e++) u.o[w][d][e][lane] = o[g][d][e];
+        __syncthreads();
+        float M = -INFINITY, lt = 0.0f, wt[NW];
+#pragma unroll
+        for (int y = 0; y < NW; y++) M = fmaxf(M, s_ml[y][0][lane]);
+#pragma unroll
+        for (int y = 0; y < NW; y++) {
+            const float my = s_ml[y][0][lane], ly = s_ml[y][1][lane];
+            // (a part whose scores are all NaN has no maximum, but its sum counts)
+            wt[y] = my == -INFINITY ? (ly != 0.0f ? 1.0f : 0.0f) : exp2f(my - M);
+            lt += ly * wt[y];
         }
-    }
-    if (w == 0 && q == 0 && row_ok) {
-        const float lse2 = lt == 0.0f ? -INFINITY : M + log2f(lt);
-        if (!whole) a.part_lse[prow] = lse2;
-        else if (a.lse) a.lse[orow] = lse2 * kLn2;
+        const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+        const size_t prow = (size_t)x.sp * a.total_q * a.Hq + orow;
+        float* out = whole ? (float*)a.out + orow * HD : a.part_o + prow * HD;
+        for (int y = w; y < DG * 4; y += NW) {  // dims 64 (y / 4) + 16 q + 4 (y % 4) + c
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < 4; c++)
+#pragma unroll
+                for (int z = 0; z < NW; z++) v[c] += u.o[z][y / 4 * 4 + c][y % 4][lane] * wt[z];
+            const int d = 64 * (y / 4) + 16 * q + 4 * (y % 4);
+            if (row_ok && d < HD) {
+                *(f32x4*)(out + d) = v * inv;
+#pragma unroll
+                for (int c = 0; c < 4; c++) odd = __builtin_fmaf(v[c], 0.0f, odd);
+            }
+        }
+        if (w == 0 && q == 0 && row_ok) {
+            const float lse2 = lt == 0.0f ? -INFINITY : M + log2f(lt);
+            if (!whole) a.part_lse[prow] = lse2;
+            else if (a.lse) a.lse[orow] = lse2 * kLn2;
+        }
     }
     if (__syncthreads_or(odd != odd) && w == 0)
         redo_rows<float>(a, x.i, x.h, x.sp, x.row0, 0, x.M, x.q0, x.L, x.list, x.t0, x.t1, 0, HD);
@@ -970,9 +990,12 @@ hipError_t launch_window(const sv_window_desc& w, const WindowPlan& plan, const 
     else if (d.page_size >= 512 / HD) SV_WINDOW(HD, NW, NB, kSegment, FEW); \
     else SV_WINDOW(HD, NW, NB, kLane, FEW)
     if (d.dtype == SV_F32) {
-        if (d.head_dim <= 64) hipLaunchKernelGGL((window_f32_kernel<1>), grid, dim3(256), 0, stream, a);
-        else if (d.head_dim <= 128) hipLaunchKernelGGL((window_f32_kernel<2>), grid, dim3(256), 0, stream, a);
-        else hipLaunchKernelGGL((window_f32_kernel<4>), grid, dim3(256), 0, stream, a);
+        const bool two = plan.block_rows == 32;
+        if (d.head_dim > 128) hipLaunchKernelGGL((window_f32_kernel<4, 1>), grid, dim3(256), 0, stream, a);
+        else if (d.head_dim > 64 && two) hipLaunchKernelGGL((window_f32_kernel<2, 2>), grid, dim3(256), 0, stream, a);
+        else if (d.head_dim > 64) hipLaunchKernelGGL((window_f32_kernel<2, 1>), grid, dim3(256), 0, stream, a);
+        else if (two) hipLaunchKernelGGL((window_f32_kernel<1, 2>), grid, dim3(256), 0, stream, a);
+        else hipLaunchKernelGGL((window_f32_kernel<1, 1>), grid, dim3(256), 0, stream, a);
     } else if (plan.few) {
         if (d.head_dim == 128) { SV_WINDOW_PAGES(128, 4, 4, true); }
         else { SV_WINDOW_PAGES(64, 4, 4, true); }

@@ -338,9 +338,21 @@ WindowPlan plan_window(const sv_window_desc& w) {
     const sv_attn_desc& d = w.attn;
     WindowPlan p{};
     const long long rows = (long long)(d.num_q_heads / d.num_kv_heads) * d.block;
-    // bf16: 32 rows per wave. fp32: all 16 rows of a block in each of four waves.
+    // bf16: 32 rows per wave. fp32: all rows of a block in each of four waves, 16 (of which the GPU holds 768 workgroups, with
+    // 64-wide heads 1024 and above 128 512) or 32 (512 and 768). 32 rows read the keys once instead of twice, but a
+    // compute unit holds fewer of them: taken where all blocks pass in fewer rounds (64 requests of 20 rows and 8 kv-heads, windows
+    // of 512: 1 round 71 us, 2 rounds of 16 rows 96 us; 80 requests, 2 rounds either way: 120 and 102 us; 48 requests, windows of
+    // 1024, 1 round either way: 115 and 100 us).
     p.waves = d.dtype == SV_F32 || rows <= 128 ? 4 : 8;
-    p.block_rows = d.dtype == SV_F32 ? 16 : 32 * p.waves;
+    p.block_rows = 32 * p.waves;
+    long long held = d.head_dim <= 64 ? 1024 : d.head_dim <= 128 ? 768 : 512;  // fp32 workgroups
+    if (d.dtype == SV_F32) {
+        const long long lists = (long long)d.num_reqs * d.num_kv_heads, held32 = d.head_dim <= 64 ? 768 : 512;
+        const bool two = d.head_dim <= 128 && (lists * ((rows + 31) / 32) + held32 - 1) / held32 <
+                                                  (lists * ((rows + 15) / 16) + held - 1) / held;
+        p.block_rows = two ? 32 : 16;
+        if (two) held = held32;
+    }
     p.row_blocks = (int)((rows + p.block_rows - 1) / p.block_rows);
     constexpr int T = kWindowTile;
     const long long tiles = longest_list(w.window, w.sinks, d.block, d.max_kv_len);
@@ -362,7 +374,7 @@ WindowPlan plan_window(const sv_window_desc& w) {
     //   units, windows of 128: items of 2 tiles 13 us, of 4 tiles 15 us.
     long long per = tiles, most = 1;
     if (p.waves == 8) most = tiles * units < 20 * 512 ? 256 / units : 512 / units;
-    else if (d.dtype == SV_F32 && tiles >= 8) most = (d.head_dim <= 64 ? 1024 : d.head_dim <= 128 ? 768 : 512) / units;
+    else if (d.dtype == SV_F32 && tiles >= 8) most = held / units;
     else if (units < 192 || (d.dtype == SV_BF16 && tiles >= 32)) most = 512 / units;
     if (d.kv_split > 0) per = std::max<long long>(1, d.kv_split / T);
     else if (most > 1) per = std::max<long long>(d.dtype == SV_F32 ? 2 : 4, (tiles + most - 1) / most);

@@ -114,6 +114,24 @@ def test_fp32_head_dims(dev, d):
     check(make(dev, 3, [4, 1], [150, 20], 6, 2, d, 16, "f32", 70, 5))
 
 
+@pytest.mark.parametrize("R,d", [(48, 64), (48, 36), (32, 128), (32, 100)])
+def test_fp32_blocks_of_32_rows(dev, R, d):
+    """So many blocks of 16 rows that those of 32 pass in fewer rounds; requests that fill 1 to 4 half blocks, one whose
+    visible value is infinite, a missing page."""
+    say("window fp32 rows", R, d)
+    rng = np.random.default_rng(R + d)
+    s = make(dev, 23, rng.integers(1, 17, R), rng.integers(0, 150, R), 32, 8, d, 16, "f32", 60, 3)
+    clean = check(s)[0]
+    k0, page = int(s["qo"][1]), int(s["table"][0, (int(s["kv"][0]) - 1) // 16])
+    s["vc"][page, :, (int(s["kv"][0]) - 1) % 16] = float("inf")  # of the first request's last row alone
+    got = call(s)[0].double().cpu().numpy()
+    assert np.abs(got[:k0 - 1] - clean[:k0 - 1]).max(initial=0) < 1e-5 and (got[k0:] == clean[k0:]).all()
+    assert not np.isfinite(got[k0 - 1]).any()
+    s["vc"][page, :, (int(s["kv"][0]) - 1) % 16] = 1.0
+    s["table"][1, int(s["kv"][1] - 1) // 16] = -1
+    check(s)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_long_windows(dev, dtype):
     """Few rows over many keys: the window is divided. Splits given by the caller."""
