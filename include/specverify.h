@@ -368,7 +368,8 @@ typedef struct {
  * rows outside [0, total_q_max) or kv_lens[i] < k_i; kv_lens[i] above max_kv_len counts as
  * max_kv_len.
  * ws: scratch of sv_window_attn_workspace_size(desc) bytes (0 for many calls), overwritten.
- * bf16 runs on MFMA with fp32 accumulation. The same call on the same inputs gives the same
+ * bf16 runs on MFMA with fp32 accumulation, each weight in two bf16 parts (off by 2^-15 at most;
+ * sv_verify_attn rounds weights to bf16). The same call on the same inputs gives the same
  * bits, and a request's results do not depend on the other requests' lengths.
  */
 sv_status sv_window_attn(const sv_window_desc* desc, const void* q, const void* k_cache, const void* v_cache,
