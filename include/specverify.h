@@ -363,8 +363,9 @@ typedef struct {
  * Pages that hold no such key of any of the request's rows are never read: their entries of
  * page_table may be -1 (sv_release_pages gives them back). A key that a row should see but
  * whose page id is outside [0, num_pages) or whose column is outside the table counts as
- * masked; a row without any key left gets out = 0 and lse = -inf. NaN and infinities in keys and
- * values that a row does not see do not reach it. Rows that no request owns are untouched, and so are those of a request with k_i outside [1, block],
+ * masked; a row without any key left gets out = 0 and lse = -inf. NaN and infinities in keys
+ * and values that a row does not see do not change its bits. Rows that no request owns are
+ * untouched, and so are those of a request with k_i outside [1, block],
  * rows outside [0, total_q_max) or kv_lens[i] < k_i; kv_lens[i] above max_kv_len counts as
  * max_kv_len.
  * ws: scratch of sv_window_attn_workspace_size(desc) bytes (0 for many calls), overwritten.

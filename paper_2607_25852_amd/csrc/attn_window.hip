@@ -62,91 +62,51 @@ template <> struct Vec4<uint16_t> {
         *(bf16x4*)p = v;
     }
 };
-__device__ inline float load1(const float* p) { return *p; }
-__device__ inline float load1(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
-__device__ inline void store1(float* p, float f) { *p = f; }
-__device__ inline void store1(uint16_t* p, float f) { *p = f2bf(f); }
 
-// One wave: the row of query qp at position p (kv-head h, page table row pt) against tiles t, t +
-// step, .. < t1 of its request's list. Leaves the softmax state (m, l) and o[e] for dim lane + 64 e.
-// Every key is used by itself: what a row does not see is not read.
-template <typename T>
-__device__ void wave_row(const WindowArgs& a, const T* qp, const int32_t* pt, int h, int p, const KeyList& list,
-                         int t, int t1, int step, float& m, float& l, float (&o)[4]) {
-    const int lane = threadIdx.x & 63, HD = a.HD, P = 1 << a.log2P;
-    m = -INFINITY, l = 0.0f;
-#pragma unroll
-    for (int e = 0; e < 4; e++) o[e] = 0.0f;
-    for (; t < t1; t += step) {
-        const int s = list_tile(list, t) * kTile + lane;
-        float z = -INFINITY;
-        size_t off = 0;
-        bool ok = s <= p && (s < a.sinks || s > p - a.window);
-        if (ok) {
-            const int col = s >> a.log2P, pg = col < a.maxp ? pt[col] : -1;
-            ok = pg >= 0 && pg < a.num_pages;
-            if (ok) {
-                off = ((((size_t)pg * a.Hkv + h) << a.log2P) + (s & (P - 1))) * HD;
-                float dot = 0.0f;
-                for (int e = 0; e < HD; e += 4) {
-                    const f32x4 x = Vec4<T>::get((const T*)a.kc + off + e), y = Vec4<T>::get(qp + e);
-                    dot += x[0] * y[0] + x[1] * y[1] + x[2] * y[2] + x[3] * y[3];
-                }
-                z = dot * a.scale;
-            }
-        }
-        float mx = z;
-        for (int x = 32; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor(mx, x, 64));
-        const float m_new = fmaxf(m, mx);
-        if (m_new == -INFINITY && !__any(ok && z != z)) continue;
-        const float alpha = m == -INFINITY ? 0.0f : expf(m - m_new);
-        const float w = ok ? expf(z - m_new) : 0.0f;
-        float ws = w;
-        for (int x = 32; x > 0; x >>= 1) ws += __shfl_xor(ws, x, 64);
-        l = l * alpha + ws;
-        m = m_new;
-#pragma unroll
-        for (int e = 0; e < 4; e++) o[e] *= alpha;
-        uint64_t todo = __ballot(ok);
-        while (todo) {
-            const int j = __builtin_ctzll(todo);
-            todo &= todo - 1;
-            const float wj = __shfl(w, j, 64);
-            const size_t offj = ((size_t)(uint32_t)__shfl((int)(off >> 32), j, 64) << 32) |
-                                (uint32_t)__shfl((int)(uint32_t)off, j, 64);
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                if (lane + 64 * e < HD) o[e] += wj * load1((const T*)a.vc + offj + lane + 64 * e);
-        }
-    }
+// Whether any of keys s0 .. s1 is seen by some rows of a request (at positions L .. last) and not by others: a key behind
+// the first row, or one that the first rows' windows begin with.
+__device__ inline bool some_shared(const WindowArgs& a, int L, int last, int s0, int s1) {
+    return (last > L) & (((s1 > L) & (s0 <= last)) | ((s1 > L - a.window) & (s0 <= last - a.window) & (s1 >= a.sinks)));
 }
-
-// Rows r0 .. r1-1 of a row block once more, one by one, by one wave: dims d0 .. d1-1, and the sum with d0 = 0. A
-// value that is not finite reaches every row of its tile (0 * inf), those too that do not see it, so
-// the rows of a wave that finds such a result are done again from the definition. So are those whose
-// scores are so large (2^31 and up) that the maximum's own rounding left no weight.
-template <typename T>
-__device__ __forceinline__ void redo_rows(const WindowArgs& a, int i, int h, int sp, int row0, int r0, int r1, int q0, int L,
-                                          const KeyList& list, int t0, int t1, int d0, int d1) {
-    const int lane = threadIdx.x & 63, HD = a.HD;
-    for (int r = r0; r < r1; r++) {
-        const int rr = row0 + r, jq = rr / a.G, head = h * a.G + rr % a.G;
-        const size_t orow = (size_t)(q0 + jq) * a.Hq + head;
-        float o[4], m, l;
-        wave_row<T>(a, (const T*)a.q + orow * HD, a.page_table + (size_t)i * a.maxp, h, L + jq, list, t0, t1, 1, m, l, o);
-        const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-        const bool whole = a.splits == 1 || t1 - t0 == list.nt;
-        const size_t prow = (size_t)sp * a.total_q * a.Hq + orow;
-        for (int e = 0; e < 4; e++) {
-            const int d = lane + 64 * e;
-            if (d < d0 || d >= d1) continue;
-            if (whole) store1((T*)a.out + orow * HD + d, o[e] * inv);
-            else a.part_o[prow * HD + d] = o[e] * inv;
+// There are at most 15 of either (a block has 16 rows). A value of theirs that is not finite must not meet the weights 0 of
+// the rows that do not see it (0 * NaN is NaN), so it is taken for 0 and its key's bit set; the rows that do see it
+// get it at the end. All other values that are not finite are seen by every row of the request, whose results they are.
+// Against no such check at all: 4 requests of one token 14.8 and 14.1 us, 64 requests of up to 16 60.2 and 58.5 us; with a
+// NaN in every request's last value 70 us (its rows computed again one by one: 28.5 ms).
+static_assert(SV_MAX_BLOCK <= 16, "bits of the keys");
+__device__ inline uint32_t shared_bit(const WindowArgs& a, int L, int s) {
+    return 1u << (s > L ? s - L - 1 : 16 + s - (L - a.window + 1));
+}
+// infinity or NaN
+__device__ inline bool odd(float x) { return (__float_as_uint(x) & 0x7F800000u) == 0x7F800000u; }
+__device__ inline bool odd(uint16_t x) { return (x & 0x7F80u) == 0x7F80u; }
+// The values of the keys `bits` to the result of the row at position p, which is at out: to 4 dims each from d on, in steps
+// of `step` below d1. Of bf16 values those that are not finite were taken for 0, of fp32 ones all. lse2 is the row's
+// in the log2 domain. Rolled loops: this is cold, and unrolled it cost a call of a few microseconds half a microsecond.
+template <typename T, typename O>
+__device__ __forceinline__ void give_back(const WindowArgs& a, uint32_t bits, const T* q, O* out, const int32_t* pt, int h, int L,
+                                          int p, float lse2, int d, int d1, int step) {
+    for (; bits; bits &= bits - 1) {
+        const int b = __builtin_ctz(bits), s = b < 16 ? L + 1 + b : L - a.window + 1 + (b - 16);
+        if (s > p || (s >= a.sinks && s <= p - a.window)) continue;
+        const int pg = pt[s >> a.log2P];
+        if ((unsigned)pg >= (unsigned)a.num_pages) continue;
+        const size_t off = ((((size_t)pg * a.Hkv + h) << a.log2P) + (s & ((1 << a.log2P) - 1))) * a.HD;
+        float z = 0.0f;
+#pragma unroll 1
+        for (int e = 0; e < a.HD; e += 4) {
+            const f32x4 x = Vec4<T>::get((const T*)a.kc + off + e), y = Vec4<T>::get(q + e);
+            z += x[0] * y[0] + x[1] * y[1] + x[2] * y[2] + x[3] * y[3];
         }
-        if (d0 == 0 && lane == 0) {
-            const float lse = l == 0.0f ? -INFINITY : m + logf(l);
-            if (!whole) a.part_lse[prow] = lse * kLog2e;
-            else if (a.lse) a.lse[orow] = lse;
+        const float weight = exp2f(z * a.scale_log2 - lse2);
+#pragma unroll 1
+        for (int e = d; e < d1; e += step) {
+            const f32x4 v = Vec4<T>::get((const T*)a.vc + off + e);
+            f32x4 o = Vec4<O>::get(out + e);
+#pragma unroll
+            for (int c = 0; c < 4; c++)
+                if (sizeof(T) == 4 || odd(v[c])) o[c] += weight * v[c];
+            Vec4<O>::put(out + e, o);
         }
     }
 }
@@ -226,8 +186,10 @@ __global__ __launch_bounds__(256, DG * RG >= 4 ? 2 : 3) void window_f32_kernel(W
         float o[NW][DG * 4][4][64];
     } u;
     __shared__ float s_ml[NW][2][64];
+    __shared__ uint32_t s_odd;  // keys whose values were taken for 0 (shared_bit)
     Item x;
     if (!find_item(a, 16 * RG, x)) return;
+    if (threadIdx.x == 0) s_odd = 0;
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int n = lane & 15, q = lane >> 4, HD = a.HD;
     const int32_t* __restrict__ pt = a.page_table + (size_t)x.i * a.maxp;
@@ -276,16 +238,20 @@ __global__ __launch_bounds__(256, DG * RG >= 4 ? 2 : 3) void window_f32_kernel(W
             kf[b] = pg >= 0 && d < HD ? *(const f32x4*)(kp + d) : f32x4{0.f, 0.f, 0.f, 0.f};
         }
         int vpg[4];
+        auto load_v = [&](unsigned gone) {  // gone: keys (by e) whose value is taken for 0
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            vpg[e] = __shfl(pg, 4 * q + e, 64);
-            const float* vp = (const float*)a.vc + row_at(max(vpg[e], 0), 4 * q + e);
+            for (int e = 0; e < 4; e++) {
+                const float* vp = (const float*)a.vc + row_at(max(vpg[e], 0), 4 * q + e);
 #pragma unroll
-            for (int c = 0; c < DG; c++) {
-                const int d = 64 * c + 4 * n;
-                vf[e][c] = vpg[e] >= 0 && d < HD ? *(const f32x4*)(vp + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int c = 0; c < DG; c++) {
+                    const int d = 64 * c + 4 * n;
+                    vf[e][c] = vpg[e] >= 0 && d < HD && !(gone >> e & 1) ? *(const f32x4*)(vp + d) : f32x4{0.f, 0.f, 0.f, 0.f};
+                }
             }
-        }
+        };
+#pragma unroll
+        for (int e = 0; e < 4; e++) vpg[e] = __shfl(pg, 4 * q + e, 64);
+        load_v(0);
         const bool any = __any(pg >= 0);
         pg = next;
         if (!any) continue;
@@ -323,6 +289,25 @@ __global__ __launch_bounds__(256, DG * RG >= 4 ? 2 : 3) void window_f32_kernel(W
                 sum += s[e];
             }
             l[g] = l[g] * alpha + sum;
+            if (g == 0 && some_shared(a, x.L, x.last, s0, s0 + 15)) {
+                unsigned gone = 0;
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int key = s0 + 4 * q + e;
+                    bool take = false;
+#pragma unroll
+                    for (int c = 0; c < DG; c++)
+#pragma unroll
+                        for (int y = 0; y < 4; y++) take |= odd(vf[e][c][y]);
+                    take &= some_shared(a, x.L, x.last, key, key);
+                    if ((__ballot(take) >> (16 * q) & 0xFFFF) != 0) {  // in any lane of the key
+                        gone |= 1u << e;
+                        if (n == 0) atomicOr(&s_odd, shared_bit(a, x.L, key));
+                    }
+                }
+                // (loaded again rather than changed in place, which costs registers)
+                if (__builtin_expect(__any(gone != 0), 0)) load_v(gone);
+            }
 #pragma unroll
             for (int d = 0; d < DG * 4; d++) o[g][d] *= alpha;
 #pragma unroll
@@ -334,7 +319,6 @@ __global__ __launch_bounds__(256, DG * RG >= 4 ? 2 : 3) void window_f32_kernel(W
     }
     // merge the waves' states; wave w finishes every fourth block of 16 dims
     const bool whole = a.splits == 1 || x.t1 - x.t0 == x.list.nt;
-    float odd = 0.0f;  // NaN where a result is not finite
 #pragma unroll
     for (int g = 0; g < RG; g++) {
         if (g > 0 && x.M <= 16 * g) break;
@@ -360,7 +344,7 @@ __global__ __launch_bounds__(256, DG * RG >= 4 ? 2 : 3) void window_f32_kernel(W
             wt[y] = my == -INFINITY ? (ly != 0.0f ? 1.0f : 0.0f) : exp2f(my - M);
             lt += ly * wt[y];
         }
-        const float inv = lt == 0.0f ? 0.0f : 1.0f / lt;
+        const float inv = 1.0f / lt;
         const size_t prow = (size_t)x.sp * a.total_q * a.Hq + orow;
         float* out = whole ? (float*)a.out + orow * HD : a.part_o + prow * HD;
         for (int y = w; y < DG * 4; y += NW) {  // dims 64 (y / 4) + 16 q + 4 (y % 4) + c
@@ -370,20 +354,16 @@ __global__ __launch_bounds__(256, DG * RG >= 4 ? 2 : 3) void window_f32_kernel(W
 #pragma unroll
                 for (int z = 0; z < NW; z++) v[c] += u.o[z][y / 4 * 4 + c][y % 4][lane] * wt[z];
             const int d = 64 * (y / 4) + 16 * q + 4 * (y % 4);
-            if (row_ok && d < HD) {
-                *(f32x4*)(out + d) = v * inv;
-#pragma unroll
-                for (int c = 0; c < 4; c++) odd = __builtin_fmaf(v[c], 0.0f, odd);
-            }
+            if (row_ok && d < HD) *(f32x4*)(out + d) = lt == 0.0f ? f32x4{0.f, 0.f, 0.f, 0.f} : v * inv;
         }
+        const float lse2 = lt == 0.0f ? -INFINITY : M + log2f(lt);
+        if (__builtin_expect(s_odd != 0 && row_ok && lt != 0.0f, 0))
+            give_back<float>(a, s_odd, (const float*)a.q + orow * HD, out, pt, x.h, x.L, p[g], lse2, 16 * q + 4 * w, HD, 64);
         if (w == 0 && q == 0 && row_ok) {
-            const float lse2 = lt == 0.0f ? -INFINITY : M + log2f(lt);
             if (!whole) a.part_lse[prow] = lse2;
             else if (a.lse) a.lse[orow] = lse2 * kLn2;
         }
     }
-    if (__syncthreads_or(odd != odd) && w == 0)
-        redo_rows<float>(a, x.i, x.h, x.sp, x.row0, 0, x.M, x.q0, x.L, x.list, x.t0, x.t1, 0, HD);
 }
 
 // ---------------------------------------------------------------------------------
@@ -427,6 +407,7 @@ struct WindowLds {
     float ml[NW][2][64];
     int32_t pid[kPageSlots];
     int32_t holes;  // a page that the list needs is missing
+    uint32_t odd;   // keys with values that were taken for 0 (shared_bit)
 };
 
 // wait until at most min(newer, MAX) tiles of IPW loads each are outstanding
@@ -470,7 +451,7 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
         }
         if (hole) lds.holes = 1;
     };
-    if (tid == 0) lds.holes = 0;
+    if (tid == 0) lds.holes = 0, lds.odd = 0;
 
     const int rg = w / PARTS, th = w % PARTS;
     // with PARTS = 4 a step takes two tiles: the wave's tile of the step, and its half of that tile
@@ -510,6 +491,7 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
 #pragma unroll
     for (int t = 0; t < DT; t++) o[t] = f32x16{};
     float m_run = -INFINITY, l_run = 0.0f;  // log2 domain
+    bool far = false;                       // an m_run of the wave is 2^28 or further from 0
 
     // DMA: wave w moves segments w*IPW .. +IPW-1 of the 2*NSEG of a tile (K first). Lane l of a segment moves
     // position l % CPR of token row seg*TPS + l/CPR, fetching chunk (l % CPR) ^ swz(token). A missing
@@ -597,18 +579,33 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
         }
     };
 
-    // before the barrier that publishes an edge tile, the lanes that copied V rows which no row sees zero them: P is
-    // 0 there, but 0 * NaN is not
+    // Before the barrier that publishes an edge tile, the lanes that copied V rows zero those that no row sees, and of those
+    // that only some rows see what is not finite (shared_bit).
     auto clean_tile = [&](int t, int c0, int buf, int edge) {
         const int tb = list_tile(list, t) * kTile;
-#pragma unroll
+#pragma unroll 1
         for (int k = 0; k < IPW; k++) {
             const int s0 = tb + (seg0 + k) * TPS, s1 = s0 + TPS - 1;  // the segment's keys
-            if (edge == 1 && (s1 <= last) & ((s1 < a.sinks) | (s0 > L - a.window))) continue;
+            const bool shared = some_shared(a, L, last, s0, s1);
+            if (edge == 1 && !shared && (s1 <= last) & ((s1 < a.sinks) | (s0 > L - a.window))) continue;
             const int s = tb + token(k);
+            u16x8* at = (u16x8*)((char*)lds.v[buf] + (seg0 + k) * 1024 + 16 * lane);
             bool zero = (s > last) | ((s >= a.sinks) & (s <= L - a.window));
             if (edge == 2) zero |= lds.pid[((t - c0) << log2T) + (token(k) >> log2S)] < 0;
-            if (zero) *(u16x8*)((char*)lds.v[buf] + (seg0 + k) * 1024 + 16 * lane) = u16x8{};
+            if (zero) *at = u16x8{};
+            if (!shared) continue;
+            // an exponent of ones carries into the sign bit's place
+            const u32x4 x = *(const u32x4*)at;
+            unsigned any = 0;
+#pragma unroll
+            for (int e = 0; e < 4; e++) any |= (x[e] & 0x7F807F80u) + 0x00800080u;
+            if (__builtin_expect((any & 0x80008000u) != 0 && some_shared(a, L, last, s, s), 0)) {
+                u16x8 v = *at;
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[e] = odd(v[e]) ? 0 : v[e];
+                *at = v;
+                atomicOr(&lds.odd, shared_bit(a, L, s));
+            }
         }
     };
 
@@ -667,8 +664,9 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
                     }
             }
         }
-        // the row's maximum: lane-local, then across the lane halves; the running maximum moves only when a
-        // score passes it by more than 8 in log2 units, so the weights stay below 2^8
+        // The row's maximum: lane-local, then across the lane halves. Weights are relative to m_run, which lies 8 (log2
+        // units) above a maximum and moves only when a score of the row passes it, so they stay at 1 or below, and no row's
+        // bits depend on another's scores.
         float mx = fmaxf(fmaxf(s[0][0], s[0][1]), s[0][2]);
 #pragma unroll
         for (int e = 3; e < 15; e += 2) mx = fmaxf(fmaxf(mx, s[0][e]), s[0][e + 1]);
@@ -682,15 +680,31 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
             mx = fmaxf(__uint_as_float(sw2[0]), __uint_as_float(sw2[1]));
         }
         mx *= a.scale_log2;
-        if (__any(mx > m_run + 8.0f)) {  // (from -inf: the first visible key)
-            const float m_new = fmaxf(m_run, mx);
+        if (__any(mx > m_run)) {  // (from -inf: the first visible key)
+            const float m_new = mx > m_run ? mx + 8.0f : m_run;
+            far = __any(fabsf(m_new) >= 0x1p28f && m_new != -INFINITY);
             const float alpha = m_run == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run - m_new);
             l_run *= alpha;
 #pragma unroll
             for (int t2 = 0; t2 < DT; t2++) o[t2] *= alpha;
             m_run = m_new;
         }
-        const float nm = m_run == -INFINITY ? 0.0f : -m_run;
+        float nm = m_run == -INFINITY ? 0.0f : -m_run, factor = a.scale_log2;
+        // A score's product with the scale is not rounded before m_run, which is, is taken from it: a factor of 2^8 at most
+        // while m_run is below 2^28. Beyond, the row's scores are rounded first.
+        if (__builtin_expect(far, 0)) {
+            if (fabsf(nm) >= 0x1p28f) {
+#pragma unroll
+                for (int x = 0; x < NSB; x++)
+#pragma unroll
+                    for (int e = 0; e < 16; e++) {
+                        float z = s[x][e] * factor;
+                        asm volatile("" : "+v"(z));  // (rounded)
+                        s[x][e] = z + nm;
+                    }
+                nm = 0.0f, factor = 1.0f;
+            }
+        }
         // O^T += V^T P^T: products j (of both parts of the weights) of half j / NJ, 16-key chunk (j % NJ) / DT, d-tile j % DT
         constexpr int NJ = 2 * DT, NT = NSB * NJ, VPD = 4;
         auto vread = [&](int j) {
@@ -708,7 +722,7 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
         float psum[NSB];
         bf16x8 phi[NSB][2], plo[NSB][2];
         auto weight = [&](int x, int e) {
-            s[x][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], a.scale_log2, nm));
+            s[x][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[x][e], factor, nm));
             psum[x] += s[x][e];
         };
         // the weights of half x as hi + lo. 2^-20 of hi is left in lo: with lo = 0 an infinite value would give 0 * inf.
@@ -856,8 +870,9 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
     const int r2 = row0 + min(rg * 32 + (tid2 & 31), M - 1), half2 = (tid2 >> 5) & 1;
     const size_t orow = (size_t)(q0 + r2 / a.G) * a.Hq + h * a.G + r2 % a.G;
     if (active && row_ok) {
-        const float inv = l_tot == 0.0f ? 0.0f : 1.0f / l_tot;
+        const float inv = 1.0f / l_tot;
         const bool whole = a.splits == 1 || t1 - t0 == list.nt;
+        const int d0 = PARTS > 1 ? th * DO * 32 : 0, d1 = PARTS > 1 ? min(d0 + DO * 32, HD) : HD;  // this wave's dims
         // dims 32 t + 8 g + 4 half .. + 3
         auto each = [&](auto put) {
 #pragma unroll
@@ -867,36 +882,29 @@ __device__ __forceinline__ void window_item(const WindowArgs& a, WindowLds<HD, N
                 for (int g = 0; g < 4; g++) {
                     f32x4 v;
 #pragma unroll
-                    for (int e = 0; e < 4; e++) v[e] = o[t][4 * g + e] * inv;
+                    for (int e = 0; e < 4; e++) v[e] = l_tot == 0.0f ? 0.0f : o[t][4 * g + e] * inv;
                     put(t * 32 + 8 * g, v);
                 }
             }
         };
-        const float lse2 = l_tot == 0.0f ? -INFINITY : m_run + __log2f(l_tot);
+        const float lse2 = l_tot == 0.0f ? -INFINITY : (m_run - 8.0f) + __log2f(256.0f * l_tot);
         if (whole) {
             uint16_t* out = (uint16_t*)a.out + orow * HD + 4 * half2;
             each([&](int d, f32x4 v) { Vec4<uint16_t>::put(out + d, v); });
+            if (__builtin_expect(lds.odd != 0 && l_tot != 0.0f, 0))
+                give_back(a, lds.odd, (const uint16_t*)a.q + orow * HD, out - 4 * half2, pt, h, L, L + r2 / a.G, lse2,
+                          d0 + 4 * half2, d1, 8);
             if (a.lse && half2 == 0 && th == 0) a.lse[orow] = lse2 * kLn2;
         } else {
             const size_t prow = (size_t)sp * a.total_q * a.Hq + orow;
             float* out = a.part_o + prow * HD + 4 * half2;
             each([&](int d, f32x4 v) { Vec4<float>::put(out + d, v); });
+            if (__builtin_expect(lds.odd != 0 && l_tot != 0.0f, 0))
+                give_back(a, lds.odd, (const uint16_t*)a.q + orow * HD, out - 4 * half2, pt, h, L, L + r2 / a.G, lse2,
+                          d0 + 4 * half2, d1, 8);
             if (half2 == 0 && th == 0) a.part_lse[prow] = lse2;
         }
     }
-    float odd = 0.0f;  // NaN where a result is not finite, or no weight is left
-    if (active && row_ok) {
-        if (m_run != -INFINITY && !(l_tot > 0.0f && l_tot < INFINITY)) odd = NAN;
-#pragma unroll
-        for (int t = 0; t < DT; t++) {
-            if (PARTS > 1 && t / DO != th) continue;
-#pragma unroll
-            for (int e = 0; e < 16; e++) odd = __builtin_fmaf(o[t][e], 0.0f, odd);
-        }
-    }
-    if (__any(odd != odd))
-        redo_rows<uint16_t>(a, i, h, sp, row0, rg * 32, min(M, rg * 32 + 32), q0, L, list, t0, t1, PARTS > 1 ? th * DO * 32 : 0,
-                      PARTS > 1 ? min((th + 1) * DO * 32, HD) : HD);
 }
 
 // FEW: at most 32 rows (of every request)
