@@ -213,6 +213,15 @@ def _rows_ptr(t, stride: int, name: str) -> int:
     return t.data_ptr()
 
 
+def _frequencies_ptr(t, pairs: int) -> int:
+    """Device pointer of inv_freq: the library reads `pairs` doubles, and model code often holds floats."""
+    if isinstance(t, int):
+        return t
+    if not (t.is_floating_point() and t.itemsize == 8) or t.numel() < pairs:
+        raise ValueError(f"inv_freq: {t.numel()} elements of {t.dtype}; {pairs} of torch.float64 are needed")
+    return _ptr(t)
+
+
 def _stream(stream) -> Optional[int]:
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
@@ -456,7 +465,7 @@ def rope_append(desc: RopeDesc, q, k_new, v_new, positions, inv_freq, page_table
     inv_freq [rot_dim / 2] float64."""
     _run(load().sv_rope_append, desc, q_out, stream, _rows_ptr(q, desc.q_stride, "q"),
          _rows_ptr(k_new, desc.k_stride, "k_new"), _rows_ptr(v_new, desc.v_stride, "v_new"), _ptr(positions),
-         _ptr(inv_freq), _ptr(page_table), _ptr(qo_indptr), _ptr(ctx_lens), _ptr(q_out), _ptr(k_cache), _ptr(v_cache))
+         _frequencies_ptr(inv_freq, desc.rot_dim // 2), _ptr(page_table), _ptr(qo_indptr), _ptr(ctx_lens), _ptr(q_out), _ptr(k_cache), _ptr(v_cache))
 
 
 # ------------------------------------------------------------------------------------
