@@ -222,24 +222,31 @@ def _frequencies_ptr(t, pairs: int) -> int:
     return _ptr(t)
 
 
-def _stream(stream) -> Optional[int]:
+_current_stream = None  # device -> handle of its current stream
+
+
+def _stream(stream, dev: int) -> Optional[int]:
+    global _current_stream
     if stream is not None:
         return stream if isinstance(stream, int) else stream.cuda_stream
-    import torch
-    # (the handle alone: building a Stream object takes longer than many of the calls)
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    if _current_stream is None:
+        import torch
+        # (the handle alone where torch has that: building a Stream object takes longer than many of the calls)
+        _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _current_stream(dev)
 
 
 def _run(fn, desc, like, stream, *args):
-    """fn(desc, *args, stream) on the device of tensor `like`: its current stream unless one is given."""
+    """fn(desc, *args, stream) on the device of tensor `like`: its current stream unless one is given. Without a
+    tensor there (a plain pointer, or None, which the library refuses): the current device."""
     import torch
-    dev, cur = -1 if isinstance(like, int) else like.get_device(), torch.cuda.current_device()
+    dev, cur = -1 if like is None or isinstance(like, int) else like.get_device(), torch.cuda.current_device()
     if dev < 0 or dev == cur:
-        _check(fn(ctypes.byref(desc), *args,
-                  torch._C._cuda_getCurrentRawStream(cur) if stream is None else _stream(stream)))
+        _check(fn(ctypes.byref(desc), *args, _stream(stream, cur)))
         return
     with torch.cuda.device(dev):
-        _check(fn(ctypes.byref(desc), *args, _stream(stream)))
+        _check(fn(ctypes.byref(desc), *args, _stream(stream, dev)))
 
 
 def _dtype_code(t) -> int:
@@ -271,9 +278,8 @@ def budget_desc(R: int, b: int, mode: str = "cost", fixed_budget: int = 0,
 def alloc_budget(desc: BudgetDesc, conf, keep, qo_indptr, sel, scores=None, utility=None, stream=None):
     """sv_alloc_budget on torch device tensors (conf [R, b-1] fp32; outputs int32 /
     fp32 / int64-for-uint64)."""
-    st = load().sv_alloc_budget(ctypes.byref(desc), _ptr(conf), _ptr(keep), _ptr(qo_indptr), _ptr(sel),
-                                _ptr(scores), _ptr(utility), _stream(stream))
-    _check(st)
+    _run(load().sv_alloc_budget, desc, keep, stream, _ptr(conf), _ptr(keep), _ptr(qo_indptr), _ptr(sel),
+         _ptr(scores), _ptr(utility))
 
 
 # ------------------------------------------------------------------------------------
@@ -297,40 +303,31 @@ def attn_workspace_size(desc: AttnDesc) -> int:
 def verify_attn(desc: AttnDesc, q, k_cache, v_cache, page_table, qo_indptr, kv_lens, out, lse=None,
                 ws=None, stream=None):
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = load().sv_verify_attn(ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
-                               _ptr(qo_indptr), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(ws), nbytes,
-                               _stream(stream))
-    _check(st)
+    _run(load().sv_verify_attn, desc, out, stream, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
+         _ptr(qo_indptr), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(ws), nbytes)
 
 
 def verify_attn_plan(desc: AttnDesc, qo_indptr, kv_lens, ws=None, stream=None):
     """sv_verify_attn_plan: the work plan of the bf16 path into ws."""
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = load().sv_verify_attn_plan(ctypes.byref(desc), _ptr(qo_indptr), _ptr(kv_lens), _ptr(ws), nbytes,
-                                    _stream(stream))
-    _check(st)
+    _run(load().sv_verify_attn_plan, desc, qo_indptr, stream, _ptr(qo_indptr), _ptr(kv_lens), _ptr(ws), nbytes)
 
 
 def verify_attn_run(desc: AttnDesc, q, k_cache, v_cache, page_table, qo_indptr, kv_lens, out, lse=None,
                     ws=None, stream=None):
     """sv_verify_attn_run: sv_verify_attn on the plan that ws holds."""
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = load().sv_verify_attn_run(ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
-                                   _ptr(qo_indptr), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(ws), nbytes,
-                                   _stream(stream))
-    _check(st)
+    _run(load().sv_verify_attn_run, desc, out, stream, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
+         _ptr(qo_indptr), _ptr(kv_lens), _ptr(out), _ptr(lse), _ptr(ws), nbytes)
 
 
 def prepare_round(bdesc: BudgetDesc, conf, keep, qo_indptr, sel, scores, utility, pdesc, block_tokens, ctx_lens,
                   tokens, positions, kv_lens, adesc=None, attn_ws=None, stream=None):
     """sv_prepare_round: budget, packing and (adesc given) the attention work plan in one launch."""
     nbytes = 0 if attn_ws is None else attn_ws.numel() * attn_ws.element_size()
-    st = load().sv_prepare_round(ctypes.byref(bdesc), _ptr(conf), _ptr(keep), _ptr(qo_indptr), _ptr(sel),
-                                 _ptr(scores), _ptr(utility), ctypes.byref(pdesc), _ptr(block_tokens),
-                                 _ptr(ctx_lens), _ptr(tokens), _ptr(positions), _ptr(kv_lens),
-                                 None if adesc is None else ctypes.byref(adesc), _ptr(attn_ws), nbytes,
-                                 _stream(stream))
-    _check(st)
+    _run(load().sv_prepare_round, bdesc, keep, stream, _ptr(conf), _ptr(keep), _ptr(qo_indptr), _ptr(sel),
+         _ptr(scores), _ptr(utility), ctypes.byref(pdesc), _ptr(block_tokens), _ptr(ctx_lens), _ptr(tokens),
+         _ptr(positions), _ptr(kv_lens), None if adesc is None else ctypes.byref(adesc), _ptr(attn_ws), nbytes)
 
 
 # ------------------------------------------------------------------------------------
@@ -343,9 +340,8 @@ def pack_desc(R: int, b: int, total_max: int) -> PackDesc:
 
 
 def pack_verify(desc: PackDesc, block_tokens, ctx_lens, qo_indptr, tokens, positions, kv_lens, stream=None):
-    st = load().sv_pack_verify(ctypes.byref(desc), _ptr(block_tokens), _ptr(ctx_lens), _ptr(qo_indptr),
-                               _ptr(tokens), _ptr(positions), _ptr(kv_lens), _stream(stream))
-    _check(st)
+    _run(load().sv_pack_verify, desc, tokens, stream, _ptr(block_tokens), _ptr(ctx_lens), _ptr(qo_indptr),
+         _ptr(tokens), _ptr(positions), _ptr(kv_lens))
 
 
 def append_desc(R: int, total_max: int, block: int, Hkv: int, d: int, page_size: int, max_pages_per_req: int,
@@ -357,9 +353,8 @@ def append_desc(R: int, total_max: int, block: int, Hkv: int, d: int, page_size:
 
 
 def append_kv(desc: AppendDesc, k_new, v_new, page_table, qo_indptr, ctx_lens, k_cache, v_cache, stream=None):
-    st = load().sv_append_kv(ctypes.byref(desc), _ptr(k_new), _ptr(v_new), _ptr(page_table), _ptr(qo_indptr),
-                             _ptr(ctx_lens), _ptr(k_cache), _ptr(v_cache), _stream(stream))
-    _check(st)
+    _run(load().sv_append_kv, desc, k_cache, stream, _ptr(k_new), _ptr(v_new), _ptr(page_table), _ptr(qo_indptr),
+         _ptr(ctx_lens), _ptr(k_cache), _ptr(v_cache))
 
 
 # ------------------------------------------------------------------------------------
@@ -379,30 +374,25 @@ def accept_workspace_size(desc: AcceptDesc) -> int:
 def spec_accept(desc: AcceptDesc, target, draft, draft_tokens, qo_indptr, u_accept, u_sample, accept_len,
                 out_tokens, flags=None, ws=None, stream=None):
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = load().sv_spec_accept(ctypes.byref(desc), _ptr(target), _ptr(draft), _ptr(draft_tokens),
-                               _ptr(qo_indptr), _ptr(u_accept), _ptr(u_sample), _ptr(accept_len),
-                               _ptr(out_tokens), _ptr(flags), _ptr(ws), nbytes, _stream(stream))
-    _check(st)
+    _run(load().sv_spec_accept, desc, accept_len, stream, _ptr(target), _ptr(draft), _ptr(draft_tokens),
+         _ptr(qo_indptr), _ptr(u_accept), _ptr(u_sample), _ptr(accept_len), _ptr(out_tokens), _ptr(flags), _ptr(ws),
+         nbytes)
 
 
 def spec_accept_noalloc(desc: AcceptDesc, target, draft, draft_tokens, qo_indptr, u_accept, u_sample, accept_len,
                         out_tokens, flags=None, stream=None):
     """sv_spec_accept_noalloc: the library's fixed device scratch replaces the workspace."""
-    st = load().sv_spec_accept_noalloc(ctypes.byref(desc), _ptr(target), _ptr(draft), _ptr(draft_tokens),
-                                       _ptr(qo_indptr), _ptr(u_accept), _ptr(u_sample), _ptr(accept_len),
-                                       _ptr(out_tokens), _ptr(flags), _stream(stream))
-    _check(st)
+    _run(load().sv_spec_accept_noalloc, desc, accept_len, stream, _ptr(target), _ptr(draft), _ptr(draft_tokens),
+         _ptr(qo_indptr), _ptr(u_accept), _ptr(u_sample), _ptr(accept_len), _ptr(out_tokens), _ptr(flags))
 
 
 def spec_accept_debug(desc: AcceptDesc, target, draft, draft_tokens, qo_indptr, u_accept, u_sample, accept_len,
                       out_tokens, flags, dbg_pq, dbg_row, ws=None, stream=None):
     """sv_spec_accept_debug: sv_spec_accept plus the fp32 values its decisions were taken on."""
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = load().sv_spec_accept_debug(ctypes.byref(desc), _ptr(target), _ptr(draft), _ptr(draft_tokens),
-                                     _ptr(qo_indptr), _ptr(u_accept), _ptr(u_sample), _ptr(accept_len),
-                                     _ptr(out_tokens), _ptr(flags), _ptr(dbg_pq), _ptr(dbg_row), _ptr(ws), nbytes,
-                                     _stream(stream))
-    _check(st)
+    _run(load().sv_spec_accept_debug, desc, accept_len, stream, _ptr(target), _ptr(draft), _ptr(draft_tokens),
+         _ptr(qo_indptr), _ptr(u_accept), _ptr(u_sample), _ptr(accept_len), _ptr(out_tokens), _ptr(flags),
+         _ptr(dbg_pq), _ptr(dbg_row), _ptr(ws), nbytes)
 
 
 # ------------------------------------------------------------------------------------
@@ -411,11 +401,9 @@ def spec_accept_debug(desc: AcceptDesc, target, draft, draft_tokens, qo_indptr, 
 def spec_accept_stats(desc: AcceptDesc, target, draft, draft_stats, draft_tokens, qo_indptr, u_accept, u_sample,
                       accept_len, out_tokens, flags=None, ws=None, stream=None):
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = load().sv_spec_accept_stats(ctypes.byref(desc), _ptr(target), _ptr(draft), _ptr(draft_stats),
-                                     _ptr(draft_tokens), _ptr(qo_indptr), _ptr(u_accept), _ptr(u_sample),
-                                     _ptr(accept_len), _ptr(out_tokens), _ptr(flags), _ptr(ws), nbytes,
-                                     _stream(stream))
-    _check(st)
+    _run(load().sv_spec_accept_stats, desc, accept_len, stream, _ptr(target), _ptr(draft), _ptr(draft_stats),
+         _ptr(draft_tokens), _ptr(qo_indptr), _ptr(u_accept), _ptr(u_sample), _ptr(accept_len), _ptr(out_tokens),
+         _ptr(flags), _ptr(ws), nbytes)
 
 
 def draft_stats_desc(R: int, drafts: int, V: int, dtype: int, temperature: float = 1.0) -> DraftStatsDesc:
@@ -430,9 +418,7 @@ def draft_stats_workspace_size(desc: DraftStatsDesc) -> int:
 
 def draft_stats(desc: DraftStatsDesc, draft_logits, stats, conf=None, ws=None, stream=None):
     nbytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = load().sv_draft_stats(ctypes.byref(desc), _ptr(draft_logits), _ptr(stats), _ptr(conf), _ptr(ws), nbytes,
-                               _stream(stream))
-    _check(st)
+    _run(load().sv_draft_stats, desc, stats, stream, _ptr(draft_logits), _ptr(stats), _ptr(conf), _ptr(ws), nbytes)
 
 
 # ------------------------------------------------------------------------------------
