@@ -78,6 +78,7 @@ struct CopyArgs {
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kCopyLoads = 4;                   // vectors in flight per thread
 constexpr unsigned kPiece = 256 * kCopyLoads;   // vectors per piece (16 KB)
+static_assert(kPiece * 16 == kCopyPieceBytes, "the host bounds the pieces of a copy");
 
 // Bound by HBM: every byte is read and written once, past the caches (3930 pages of 32 KB in two layers and two
 // caches, 1.03 GB: 209 us with ordinary loads and stores, 193 us so; a large plain copy runs at 4.9 TB/s). A workgroup

@@ -294,6 +294,10 @@ sv_status check_copy(const sv_copy_desc* desc) {
         return fail(SV_ERR_UNSUPPORTED, "sv_copy_pages: a page of %d heads x %lld bytes is above 2^30", d.num_kv_heads, row);
     if (d.num_layers > (1 << 16) || d.max_copies > (1 << 24) || d.num_pages > (1 << 24))
         return fail(SV_ERR_UNSUPPORTED, "sv_copy_pages: above 2^16 layers, 2^24 copies or 2^24 pages");
+    // the steps of a copy are numbered in 32 bits
+    const long long pieces = (row * d.num_kv_heads + kCopyPieceBytes - 1) / kCopyPieceBytes;
+    if (2 * d.num_layers * pieces > 0x7FFFFFFFLL)
+        return fail(SV_ERR_UNSUPPORTED, "sv_copy_pages: %d layers of pages of %lld bytes", d.num_layers, row * d.num_kv_heads);
     const long long dense = row / esz * d.num_kv_heads * d.num_pages;  // elements of a layer
     if (d.layer_stride != 0 && (d.layer_stride < dense || d.layer_stride * esz % 16 != 0 || d.layer_stride > (1LL << 50)))
         return fail(SV_ERR_INVALID_ARG, "sv_copy_pages: layer_stride %lld is below a layer's cache (%lld), or not a "

@@ -51,6 +51,7 @@ struct AcceptPlan {
     size_t off_cnt, off_stats_t, off_stats_q, off_plan, off_csum, off_tsum, total;  // off_tsum 0: none
 };
 constexpr int kPageChunkSize = 4096;  // pages per workgroup of the page calls
+constexpr int kCopyPieceBytes = 16384;  // of a page, per step of a workgroup of sv_copy_pages
 struct ReservePlan {  // offsets in int32 words
     int chunks;
     bool alone;  // one workgroup walks all pages
