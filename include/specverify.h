@@ -433,7 +433,8 @@ sv_status sv_fork_pages(const sv_pages_desc* desc, int32_t rows_in, const int32_
  * columns than the table has, and all requests after it stay as they were.
  * info [4] int32 out: requests served (a prefix of the batch), pages taken, copies, free
  * pages left. copy_src, copy_dst, copy_tokens [R] int32 out; entries past the copies untouched.
- * ws: scratch of sv_reserve_pages_workspace_size(desc) bytes. R <= 4096.
+ * ws: scratch of sv_reserve_pages_workspace_size(desc) bytes, required for every size (up to
+ * 4096 pages the call keeps its work in LDS and leaves ws as it was). R <= 4096.
  */
 sv_status sv_reserve_pages(const sv_pages_desc* desc, int32_t* page_table, int32_t* ref, const int32_t* ctx_lens,
                            const int32_t* new_lens, int32_t* copy_src, int32_t* copy_dst, int32_t* copy_tokens,

@@ -40,7 +40,7 @@ __global__ __launch_bounds__(kWalkThreads) void reserve_alone_kernel(ReserveArgs
     __shared__ ReserveLds<kWalkThreads> lds;
     __shared__ int32_t was[kPageChunk], writers[kPageChunk], last[kPageChunk], demand[kPageChunk], copy_of[kPageChunk];
     __shared__ int32_t upto[kReserveReqs], copies[kReserveReqs];
-    if (a.num_pages > kPageChunk) return;
+    if (a.num_pages > kPageChunk) return;  // (plan_reserve takes this kernel for one chunk only; the arrays above hold no more)
     for (int p = threadIdx.x; p < a.num_pages; p += kWalkThreads) was[p] = a.ref[p];
     a.was = was, a.writers = writers, a.last = last, a.demand = demand, a.copy_of = copy_of, a.upto = upto, a.copies = copies;
     __syncthreads();

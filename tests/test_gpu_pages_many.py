@@ -1,4 +1,4 @@
-"""sv_copy_pages with more steps than workgroups: every workgroup takes several (exact)."""
+"""sv_copy_pages with more steps than workgroups: every workgroup takes several (exact). The scratch of sv_reserve_pages."""
 import numpy as np
 import pytest
 
@@ -37,3 +37,16 @@ def test_copies_of_many_steps(dev, n, layers, Hkv, page, d, dtype):  # noqa: F81
                         m = page if tk is None else min(max(int(tk[e]), 0), page)
                         want[:, dst[e], :, :m] = was[:, src[e], :, :m]
                 assert dev.equal(got, want), (count, tk is None)
+
+
+@pytest.mark.parametrize("pages,kept", [(50, True), (4096, True), (4097, False)])
+def test_scratch_of_reserve(dev, pages, kept):  # noqa: F811
+    """Left as it was up to 4096 pages."""
+    from paper_2607_25852_amd import binding as B
+    say("reserve scratch", pages)
+    d = B.pages_desc(3, 4, pages, 16)
+    ws = dev.full((B.reserve_pages_workspace_size(d),), 0x77, dtype=dev.uint8, device="cuda")
+    z = lambda n: dev.zeros(n, dtype=dev.int32, device="cuda")
+    table, refs, info = dev.full((3, 4), -1, dtype=dev.int32, device="cuda"), z(pages), z(4)
+    B.reserve_pages(d, table, refs, z(3), z(3) + 20, z(3), z(3), z(3), info, ws)
+    assert info.tolist() == [3, 6, 0, pages - 6] and bool((ws == 0x77).all()) == kept
