@@ -115,8 +115,8 @@ __device__ __forceinline__ void give_back(const WindowArgs& a, uint32_t bits, co
 // kv-head)s, whose heads share pages, and the row blocks of one follow each other. With by_rows (blocks of up to 64
 // requests) the requests with the most rows come first and are dealt to the XCDs in turn, so that all XCDs have as
 // much to do and the last items are short ones. Requests of 1 to 16 positions, in their own order and by rows:
-// 32 with windows of 32768 (512 items of 8 waves, 256 at a time) 488 and 458 us, 48 with windows of 4000
-// (384 items, all at once) 126 and 112 us, 64 with windows of 1024 55.3 and 54.3 us.
+// 32 with windows of 32768 (512 items of 8 waves, 256 at a time) 630 and 584 us, 48 with windows of 4000
+// (384 items, all at once) 183 and 157 us, 64 with windows of 1024 66.6 and 61.8 us.
 struct Item {
     int i, h, sp, row0, M;  // request, kv-head, split, first row of the kv-head group, rows
     int q0, L, last;        // the request's first row; positions of its first and last row
@@ -383,11 +383,11 @@ __global__ __launch_bounds__(256, DG * RG >= 4 ? 2 : 3) void window_f32_kernel(W
 // (rms, relative, against 64 bits) instead of the 0.0017 that their own rounding costs; that form took 54.0 instead of 56.6 us for
 // 64 requests with windows of 1024 and, where the products bound it (32 requests, windows of 32768), 465 instead of 575 us.
 // Maximum, sum (of the fp32 weights) and outputs stay in fp32.
-// Bound: 64 requests of 1 to 16 rows, 8 kv-heads of 128 dims, windows of 1024 (282 MB, two waves on 32 rows): 54 us,
-// 5.3 TB/s, of which 6 us go by before the first tile is there (packing, page ids, first copies).
-// 32 requests, 16 heads per kv-head, windows of 32768 (2.16 GB, waves with whole tiles): 450 us, 4.8 TB/s, the
-// tile's dependent steps (LDS reads, exponents and products take 0.85 to 1 us each of the 1.6 us of a
-// tile). 4 requests of one row, windows of 1024 (17 MB, 5 splits): 10 us and 4 us of merge, all of it latency.
+// Bound: 64 requests of 1 to 16 rows, 8 kv-heads of 128 dims, windows of 1024 (282 MB, two waves on 32 rows): 60 us,
+// 4.7 TB/s, of which 6 us go by before the first tile is there (packing, page ids, first copies).
+// 32 requests, 16 heads per kv-head, windows of 32768 (2.16 GB, waves with whole tiles): 550 to 585 us, 3.8 TB/s, the
+// tile's dependent steps (LDS reads, exponents, and the products, 48 per wave, of which two share a matrix unit: 1.3 us of the 2 us of
+// a tile). 4 requests of one row, windows of 1024 (17 MB, 5 splits): 12 us and 3 to 4 us of merge, all of it latency.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kPageSlots = 1024;  // page ids staged at a time
 

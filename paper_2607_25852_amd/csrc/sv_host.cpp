@@ -363,15 +363,16 @@ WindowPlan plan_window(const sv_window_desc& w) {
     const long long units = (long long)d.num_reqs * d.num_kv_heads * p.row_blocks;
     // Lists are divided where the units alone leave compute units idle, into items of at least 4 tiles (fp32: 2) that
     // the GPU holds all at once: a few items more take a whole round longer (160 units of 128 rows, windows of 4000: 3
-    // splits 58 us, 4 splits 83 us). A divided list costs a second kernel (about 5 us).
-    // - bf16, 4 waves: two workgroups per compute unit, 512 items. Windows of 1024: 128 units of 128 rows take 30 us divided and
-    //   38 us whole, 256 units 43 and 37 us, 216 units of 64-wide heads 28 and 22 us; items of 2 tiles take no less
-    //   than of 4 (13.7 and 13.5 us for 32 units of 8 rows). Long lists in halves up to 256 units (256 units of 128 rows: windows
-    //   of 2000 57 us either way, of 4000 84 us, whole 96 us; 216 units, 4000, most contexts short: 54 and 83 us).
-    // - bf16, 8 waves: one workgroup per compute unit, 256 items (80 units of 256 rows, windows of 1000: 31 us, with 480 items
-    //   40 us; 160 units undivided 43 us, with 480 items 50 us). Twice as many even out what the rows differ, where items keep
-    //   20 tiles (160 units, windows of 8192: 184 us, undivided 240 us; 128 units, 32768: 482 us, with 256 items 520 us; 136
-    //   units, 5000: 113 and 153 us, 200 units, 3500: 121 and 115 us, 240 units, 2400: 100 and 87 us).
+    // splits 93 us, 4 splits 108 us). A divided list costs a second kernel (about 4 us). (All figures with full blocks and
+    // contexts beyond the window where nothing else is said.)
+    // - bf16, 4 waves: two workgroups per compute unit, 512 items. Windows of 1024: 128 units of 128 rows take 41 us divided and
+    //   45 us whole, 256 units 65 and 49 us, 216 units of 64-wide heads and 32 rows 21.5 and 20.2 us; items of 2 tiles take no less
+    //   than of 4 (14.4 and 14.6 us for 32 units of 8 rows). Long lists in halves up to 256 units (256 units of 128 rows: windows
+    //   of 2000 83 us, whole 79 us, of 4000 139 and 138 us; 216 units, 4000, most contexts short: 92 and 117 us).
+    // - bf16, 8 waves: one workgroup per compute unit, 256 items (80 units of 256 rows, windows of 1000: 41 us, with 480 items
+    //   53 us; 160 units undivided 58 us, with 480 items 71 us). Twice as many even out what the rows differ, where items keep
+    //   20 tiles (160 units, windows of 8192: 296 us, undivided 325 us; 128 units of 1 to 16 positions, 32768: 583 us, with 256 items
+    //   624 us; 136 units, 5000: 176 and 198 us; but 200 full units, 3500: 192 and 162 us, for which it is no gain).
     // - fp32: three workgroups per compute unit, four of 64-wide heads and two of heads above 128. Lists of less than 8 tiles
     //   where there are few units alone. 256 units of 16 rows, windows of 512: 27 us in 3 splits, 30 us whole; of
     //   230 (6 tiles) 20 us in 3 splits, 19 us whole; 160 units of 64-wide heads, 2000: 6 splits 31 us, 4 splits 35 us; 64
@@ -385,14 +386,14 @@ WindowPlan plan_window(const sv_window_desc& w) {
     p.split_tiles = (int)std::min(per, tiles);
     p.splits = (int)((tiles + p.split_tiles - 1) / p.split_tiles);
     // All four waves on the same 32 rows, two tiles at a time: a step takes as long as one of two waves on one tile
-    // (27 requests of 8 positions and 64-wide heads 18.8 and 22.0 us). 128-wide heads need the LDS of a whole compute
-    // unit for it, which pays where every unit has one (192 units of 8 rows, windows of 1024: 26.9 and 29.7 us, 512
-    // units 55 and 48 us) and walks its whole list (32 units in 5 splits 14.2 and 13.8 us).
+    // (27 requests of 8 positions and 64-wide heads 20.7 and 24.2 us). 128-wide heads need the LDS of a whole compute
+    // unit for it, which pays where every unit has one (192 units of 8 rows, windows of 1024: 29.6 and 31.4 us, 512
+    // units 58.7 and 49.6 us) and walks its whole list (32 units in 5 splits 15.4 and 14.6 us).
     p.few = d.dtype == SV_BF16 && rows <= 32 && (d.head_dim == 64 || (units <= 256 && p.splits == 1));
     // Where the rows may differ, every XCD gets two (request, split)s at least and there is enough to do that the
     // order repays finding it (0.5 to 1 us). Tiles in all: 128-row blocks of four waves, of which two share a compute unit,
-    // from 4096 on (3900 tiles lose 1 of 22 us, 5200 win 4 of 43, 6100 win 4 of 45); others from 8192 (four waves on 32 rows, 6400
-    // lose 1 of 25 us; eight waves, 6200 lose 2 of 60; fp32, 3600 lose 2 of 55).
+    // from 4096 on (3900 tiles lose 1 of 45 us, 5200 win 7 of 53); others from 8192 (four waves on 32 rows, 6400
+    // lose 1 of 25 us; eight waves, 6200 lose 1 of 92; fp32, 3600 lose 1 of 63).
     const bool pairs = d.dtype == SV_BF16 && p.waves == 4 && !p.few;
     p.by_rows = d.block > 1 && d.num_reqs <= 64 && (long long)d.num_reqs * p.splits >= 16 &&
                 tiles * units >= (pairs ? 4096 : 8192);
