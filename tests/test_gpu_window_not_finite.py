@@ -98,6 +98,28 @@ def test_rows_that_do_not_see_it_keep_their_bits(dev, dtype, Hq, Hkv, d, page, k
             s[name] = keep
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq", [2, 8, 16])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (4, 0), (5, 70), (16, 2), (17, 0), (1000, 0), (3, 500)])
+@pytest.mark.parametrize("ctx", [0, 1, 60, 130])
+def test_windows_shorter_than_a_block(dev, dtype, Hq, window, sinks, ctx):  # noqa: F811
+    """Every key in turn that some rows of the block see, and all second ones; short requests among the first tokens."""
+    say("window not finite, short", dtype, Hq, window, sinks, ctx)
+    s = make(dev, 44, [16, 2], [ctx, 40], Hq, 1, 64, 16, dtype, window, sinks)
+    clean = call(s)
+    keep = s["vc"].clone()
+    lo = max(0, ctx - window + 1)
+    for keys in [[lo], [ctx], [ctx + 3], [ctx + 15], list(range(lo % 2, ctx + 16, 2))]:
+        touched = np.zeros(s["total"], bool)
+        touched[:16] = sees(s, 0, keys)
+        for p in keys:
+            if s["table"][0, p // 16] >= 0 and (p < sinks or p > ctx - window):
+                pg, at = slot(s, 0, p)
+                s["vc"][pg, :, at, 5] = float("inf")
+        compare(s, touched, clean)
+        s["vc"].copy_(keep)
+
+
 @pytest.mark.parametrize("dtype,Hq,Hkv,d,page,k,split", LAYOUTS)
 def test_a_value_that_all_rows_see(dev, dtype, Hq, Hkv, d, page, k, split):  # noqa: F811
     """In the first, a middle and the last part of a list, with those that only some rows see beside it."""
